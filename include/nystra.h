@@ -308,6 +308,129 @@ int nystra_landmark_map(int N, int m, int mode, int32_t *map_host);
  * -NYSTRA_ERR_UNSUPPORTED). */
 int nystra_select_variant(int N, int d_h, int m, int dtype, const nystra_opts *opts);
 
+/* ---- Training and serving a layer: LayerNorm, dropout, differential attention ----
+ * The conventions at the top hold here too (streams, errors, no allocation, kernel
+ * launches only), except that tensors may be strided where strides are given, in
+ * elements and not negative; the innermost dimension is always contiguous.  Sums,
+ * softmax statistics and normalisation are fp32.  No result depends on the order
+ * in which workgroups run: the same call gives the same bits. */
+
+/* LayerNorm over the channels of each of `rows` rows:
+ *   mean, var = mean and (biased) variance of the row, rstd = (var + eps)^(-1/2),
+ *   y = (x - mean) rstd weight + bias.
+ * weight and bias ([channels], `dtype`) may be NULL (ones, zeros).  mean and rstd
+ * (fp32 [rows]) are stored for the backward pass, or both NULL.
+ * 0 <= rows < 2^31 (0: a no-op), 1 <= channels <= 4096, eps finite and >= 0; row strides at
+ * least `channels`.  Y must not overlap an input. */
+int nystra_layer_norm_forward(const void *X, int64_t x_stride, const void *weight,
+                              const void *bias, void *Y, int64_t y_stride, float *mean,
+                              float *rstd, int64_t rows, int channels, float eps, int dtype,
+                              void *stream);
+
+/* Its backward pass, from the mean and rstd of the forward pass:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)), g = dy weight, xh = (x - mean) rstd,
+ *   dweight = sum over rows of dy xh, dbias = sum over rows of dy (summed in fp32,
+ *   stored in `dtype`; either may be NULL).
+ * The workspace (256-byte aligned, nystra_layer_norm_workspace_size bytes, disjoint from
+ * every tensor) holds partial sums.  With rows == 0 dweight and dbias are zero.  Outputs
+ * must overlap neither inputs nor each other. */
+int nystra_layer_norm_workspace_size(int64_t rows, int channels, size_t *bytes);
+
+int nystra_layer_norm_backward(const void *dY, int64_t dy_stride, const void *X, int64_t x_stride,
+                               const void *weight, const float *mean, const float *rstd, void *dX,
+                               int64_t dx_stride, void *dweight, void *dbias, int64_t rows,
+                               int channels, int dtype, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/* Dropout of n elements from a counter-based generator, onto a residual (may be NULL):
+ *   y_i = residual_i + (r_i >= T ? x_i 65536 / (65536 - T) : 0),  T = round(65536 p),
+ * so the probability is p to within 2^-17, and the kept share is scaled by exactly its
+ * inverse (T = 65536 keeps nothing).  r_i are 16 bits of Philox-4x32 (10 rounds) with key
+ * `seed` and counter (i / 8, offset), i / 8 in its low 64 bits, as bits 16 (i % 2) .. + 15 of
+ * word (i % 8) / 2: the mask depends on i, seed and
+ * offset only and is never stored.  The backward pass is the same call on dy, without
+ * residual; a dropped element's x is not read into the result (an infinity or NaN there
+ * is gone).  Give every use of one seed an offset of its own.
+ * state: NULL, or a device pointer to two uint64: the kernel then takes the seed from
+ * state[0] (and `seed` is ignored) and adds state[1] to `offset`, so that a recorded graph
+ * draws new masks when the caller changes them between replays.
+ * 0 <= n <= 2^34, 0 <= p <= 1.  Y may be X or the residual itself; any other overlap is
+ * refused.  state must be 8-byte aligned. */
+int nystra_dropout(const void *X, const void *residual, void *Y, int64_t n, float p,
+                   uint64_t seed, uint64_t offset, const uint64_t *state, int dtype,
+                   void *stream);
+
+/* Differential attention: the difference of two softmax maps over the same values,
+ *   O = (softmax(scale Q1 K1^T) - lambda_h softmax(scale Q2 K2^T)) V
+ * per window and head h, lambda fp32 [heads] (device).  Q is [n_windows][2 heads][n_q][d_qk],
+ * heads 2h and 2h + 1 being the two maps of head h, K [n_windows][2 kv_heads][n_k][d_qk]
+ * likewise, V [n_windows][kv_heads][n_k][d_v], O [n_windows][heads][n_q][d_v]; kv_heads
+ * divides heads, and head h reads the keys and values of head h / (heads / kv_heads).
+ * Each is given as a nystra_view: its data and the strides of its first three dimensions.
+ *
+ * Keys.  kv_len (device int32 [n_windows], clamped to 0 .. n_k) gives every window a length
+ * of its own; NULL: n_k.  Keys and values at or behind it are not read.  causal:
+ *   NYSTRA_CAUSAL_NONE   every query sees all keys below the length;
+ *   NYSTRA_CAUSAL_START  query i sees keys 0 .. i (a batch padded at its end);
+ *   NYSTRA_CAUSAL_END    query i sees keys 0 .. length - n_q + i: the queries are the
+ *                        last n_q tokens of the sequence (new tokens over a cache).
+ * A query that sees no key gets zeros, and passes no gradient.  Inside the length, keys and
+ * values that a causal query does not see must be finite.
+ *
+ * Arithmetic.  Scores, softmax and accumulation are fp32.  fp32 runs on the fp32 matrix
+ * cores; bf16 on the bf16 ones, with the probabilities (in the backward pass also the
+ * gradients of the scores) rounded to bf16 for the products that take them.
+ *
+ * For training, lse (fp32 [n_windows][2 heads][n_q], base-2 logarithms of the softmax
+ * sums; -infinity for a query without keys) and, where n_k > NYSTRA_DIFF_SHORT_KEYS, O2
+ * ([n_windows][heads][n_q][d_v] in `dtype`, the second map's output) are stored for the
+ * backward pass; both are contiguous, and NULL for inference.  O2 is NULL for shorter n_k.
+ *
+ * Backward: dQ, dK, dV in `dtype` (dK, dV summed over the heads that share them, zero at or
+ * behind the length) and dlambda (fp32 [heads]) from dO and the same inputs, O, O2 and lse.
+ *
+ * Limits: n_windows >= 0 (0: forward is a no-op, backward writes zeros to dlambda),
+ * 1 <= kv_heads <= heads, 1 <= n_q, n_k <= 2^20, 1 <= d_qk <= 64, 1 <= d_v <= 128, scale
+ * finite (<= 0: 1/sqrt(d_qk)), fewer than 2^24 rows (window, head, query) and fewer than
+ * 2^24 tiles of 32 keys.  Outputs must not overlap inputs, nor themselves or each other
+ * (dQ, dK and dV may lie side by side in one buffer).
+ * The workspaces (nystra_diff_attn_workspace_size, 256-byte aligned, disjoint from every
+ * tensor; the forward one 0 bytes unless the keys are split over workgroups) hold
+ * intermediate sums; calls that may run concurrently need distinct ones. */
+typedef enum {
+    NYSTRA_CAUSAL_NONE = 0,
+    NYSTRA_CAUSAL_START = 1,
+    NYSTRA_CAUSAL_END = 2
+} nystra_causal;
+
+#define NYSTRA_DIFF_SHORT_KEYS 128
+
+typedef struct nystra_view {
+    void *data;
+    int64_t window, head, token;   /* strides in elements */
+} nystra_view;
+
+typedef struct nystra_diff_shape {
+    int n_windows, heads, kv_heads, n_q, n_k, d_qk, d_v;
+    int causal;    /* nystra_causal */
+    float scale;
+} nystra_diff_shape;
+
+int nystra_diff_attn_workspace_size(const nystra_diff_shape *shape, int backward, int dtype,
+                                    size_t *bytes);
+
+int nystra_diff_attn_forward(const nystra_view *Q, const nystra_view *K, const nystra_view *V,
+                             const float *lambda, const int32_t *kv_len, const nystra_view *O,
+                             void *O2, float *lse, const nystra_diff_shape *shape, int dtype,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+int nystra_diff_attn_backward(const nystra_view *dO, const nystra_view *Q, const nystra_view *K,
+                              const nystra_view *V, const float *lambda, const int32_t *kv_len,
+                              const nystra_view *O, const void *O2, const float *lse,
+                              const nystra_view *dQ, const nystra_view *dK, const nystra_view *dV,
+                              float *dlambda, const nystra_diff_shape *shape, int dtype,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static description of a status code. */
 const char *nystra_status_str(int status);
 

@@ -19,5 +19,12 @@ from .binding import (  # noqa: F401
     nystra_select_variant,
     nystra_status_str,
     nystra_default_opts,
+    nystra_layer_norm_forward,
+    nystra_layer_norm_backward,
+    nystra_layer_norm_workspace_size,
+    nystra_dropout,
+    nystra_diff_attn_forward,
+    nystra_diff_attn_backward,
+    nystra_diff_attn_workspace_size,
     make_opts,
 )

@@ -6,6 +6,7 @@ the attention is computed here, and there is no fallback: if libnystra.so is
 missing or a call fails, a NystraError is raised.
 """
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -25,9 +26,14 @@ EXPORTS = (
     "nystra_block_workspace_size", "nystra_block_forward", "nystra_attn_forward_noalloc",
     "nystra_block_packed_size", "nystra_block_pack_weights", "nystra_block_forward_packed",
     "nystra_layer_forward", "nystra_status_str", "nystra_last_error",
+    "nystra_layer_norm_forward", "nystra_layer_norm_workspace_size", "nystra_layer_norm_backward",
+    "nystra_dropout", "nystra_diff_attn_workspace_size", "nystra_diff_attn_forward",
+    "nystra_diff_attn_backward",
 )
 STATIC_SCRATCH_BYTES = 32 << 20   # NYSTRA_STATIC_SCRATCH_BYTES
 BLOCK_NYSTROM, BLOCK_EXACT = 0, 1
+CAUSAL_NONE, CAUSAL_START, CAUSAL_END = 0, 1, 2
+DIFF_SHORT_KEYS = 128             # NYSTRA_DIFF_SHORT_KEYS
 
 
 class NystraError(RuntimeError):
@@ -55,6 +61,16 @@ class LayerParams(ctypes.Structure):
 class Opts(ctypes.Structure):
     _fields_ = [("pinv_iters", ctypes.c_int), ("landmark_mode", ctypes.c_int),
                 ("scale", ctypes.c_float), ("variant", ctypes.c_int)]
+
+
+class View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("window", "head",
+                                                                             "token")]
+
+
+class DiffShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n_windows", "heads", "kv_heads", "n_q", "n_k", "d_qk",
+                                            "d_v", "causal")] + [("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -104,6 +120,19 @@ def lib():
                                                     _vp, ctypes.POINTER(BlockShape), _i, _i,
                                                     ctypes.POINTER(Opts), _i, _vp,
                                                     ctypes.c_size_t, _vp])
+    i64, u64, size = ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
+    view, dshape = ctypes.POINTER(View), ctypes.POINTER(DiffShape)
+    L.nystra_layer_norm_forward.argtypes = ([_vp, i64, _vp, _vp, _vp, i64, _vp, _vp, i64, _i,
+                                             ctypes.c_float, _i, _vp])
+    L.nystra_layer_norm_workspace_size.argtypes = [i64, _i, ctypes.POINTER(size)]
+    L.nystra_layer_norm_backward.argtypes = ([_vp, i64, _vp, i64, _vp, _vp, _vp, _vp, i64, _vp,
+                                              _vp, i64, _i, _i, _vp, size, _vp])
+    L.nystra_dropout.argtypes = [_vp, _vp, _vp, i64, ctypes.c_float, u64, u64, _vp, _i, _vp]
+    L.nystra_diff_attn_workspace_size.argtypes = [dshape, _i, _i, ctypes.POINTER(size)]
+    L.nystra_diff_attn_forward.argtypes = ([view] * 3 + [_vp, _vp, view, _vp, _vp, dshape, _i, _vp,
+                                                         size, _vp])
+    L.nystra_diff_attn_backward.argtypes = ([view] * 4 + [_vp, _vp, view, _vp, _vp] + [view] * 3 +
+                                            [_vp, dshape, _i, _vp, size, _vp])
     for name in EXPORTS:
         if name not in ("nystra_status_str", "nystra_last_error"):
             getattr(L, name).restype = ctypes.c_int
@@ -375,3 +404,253 @@ def nystra_select_variant(N, d_h, m, dtype=F32, opts=None):
 
 def nystra_status_str(status):
     return lib().nystra_status_str(status).decode()
+
+
+# ---- training and serving a layer: LayerNorm, dropout, differential attention ----
+
+
+def _placed(f):
+    """Runs f on its first tensor's device and on `stream` (default: that device's
+    current stream).  On a stream that is not the current one everything that f
+    allocates belongs to that stream, so that nothing is reused under its kernels."""
+    name = f.__code__.co_varnames[0]
+
+    @functools.wraps(f)
+    def call(*args, stream=None, **kw):
+        import torch
+        first = args[0] if args else kw.get(name)
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+            raise ValueError(f"{f.__name__} needs device tensors")
+        if stream is None and first.device.index == torch.cuda.current_device():
+            return f(*args, **kw)
+        with torch.cuda.device(first.device):
+            if stream is None:
+                return f(*args, **kw)
+            if stream.device != first.device:
+                raise ValueError("the stream belongs to another device than the tensors")
+            with torch.cuda.stream(stream):
+                return f(*args, **kw)
+    return call
+
+
+def _raw_stream(t):
+    import torch
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _same(first, tensors, dtype=None):
+    for t in tensors:
+        if t is not None and (t.device != first.device or t.dtype != (dtype or first.dtype)):
+            raise ValueError(f"expected {dtype or first.dtype} tensors on {first.device}")
+
+
+def _vector(t, n, what):
+    if t is not None and (t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{what} must be contiguous with {n} elements")
+
+
+def _rows(t, C):
+    """The row stride of [..., C] as a list of rows (raises where there is none)."""
+    if t.is_contiguous():
+        return C
+    if C > 1 and t.stride(-1) != 1:
+        raise ValueError("the channels must be contiguous")
+    try:
+        stride = t.view(-1, C).stride(0)
+    except RuntimeError:
+        raise ValueError("the rows must lie at one stride") from None
+    return stride if t.numel() > C else C
+
+
+def _bytes(t):
+    return t.numel() * t.element_size() if t is not None else 0
+
+
+@_placed
+def nystra_layer_norm_forward(x, weight=None, bias=None, eps=1e-5, with_stats=False, out=None):
+    """LayerNorm over the last dimension of x [..., C] (rows at one stride): y, or
+    with_stats (y, mean, rstd) for the backward pass (fp32, one value to a row)."""
+    import torch
+    C = int(x.shape[-1]) if x.dim() else 0
+    code = _dtype_code(x)
+    _same(x, (weight, bias, out))
+    _vector(weight, C, "weight")
+    _vector(bias, C, "bias")
+    rows = x.numel() // max(C, 1)
+    if out is not None and out.shape != x.shape:
+        raise ValueError("out must have x's shape")
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    mean = rstd = None
+    if with_stats:
+        mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+                      for _ in range(2))
+    rc = lib().nystra_layer_norm_forward(_ptr(x), _rows(x, C), _ptr(weight), _ptr(bias), _ptr(y),
+                                         _rows(y, C), _ptr(mean), _ptr(rstd), rows, C, eps, code,
+                                         _raw_stream(x))
+    _check(rc, "nystra_layer_norm_forward")
+    return (y, mean, rstd) if with_stats else y
+
+
+def nystra_layer_norm_workspace_size(rows, channels):
+    n = ctypes.c_size_t(0)
+    _check(lib().nystra_layer_norm_workspace_size(rows, channels, ctypes.byref(n)),
+           "nystra_layer_norm_workspace_size")
+    return int(n.value)
+
+
+@_placed
+def nystra_layer_norm_backward(dy, x, weight, mean, rstd, workspace=None):
+    """(dx, dweight, dbias) of nystra_layer_norm_forward; weight may be None (ones)."""
+    import torch
+    C = int(x.shape[-1]) if x.dim() else 0
+    code = _dtype_code(x)
+    _same(dy, (x, weight))
+    _same(dy, (mean, rstd), torch.float32)
+    rows = x.numel() // max(C, 1)
+    if dy.shape != x.shape:
+        raise ValueError("dy must have x's shape")
+    _vector(weight, C, "weight")
+    _vector(mean, rows, "mean")
+    _vector(rstd, rows, "rstd")
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dw, db = torch.empty(2, C, dtype=x.dtype, device=x.device).unbind(0)
+    if workspace is None:
+        workspace = torch.empty(nystra_layer_norm_workspace_size(rows, C), dtype=torch.uint8,
+                                device=x.device)
+    _same(dy, (workspace,), workspace.dtype)
+    rc = lib().nystra_layer_norm_backward(_ptr(dy), _rows(dy, C), _ptr(x), _rows(x, C),
+                                          _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx), C,
+                                          _ptr(dw), _ptr(db), rows, C, code, _ptr(workspace),
+                                          _bytes(workspace), _raw_stream(x))
+    _check(rc, "nystra_layer_norm_backward")
+    return dx, dw, db
+
+
+@_placed
+def nystra_dropout(x, p, seed=0, offset=0, state=None, residual=None, out=None):
+    """residual + dropout(x) of contiguous tensors.  The mask follows from the
+    element's index, `seed` and `offset` (non-negative, below 2^64): the same call on the
+    gradient, without residual, is the backward pass.  `state`: int64 [2] on the device
+    in place of the seed and added to the offset (for recorded graphs)."""
+    import torch
+    code = _dtype_code(x)
+    _same(x, (residual, out))
+    for t in (x, residual, out):
+        if t is not None and (t.shape != x.shape or not t.is_contiguous()):
+            raise ValueError("x, residual and out must be contiguous and of one shape")
+    if state is not None:
+        _same(x, (state,), torch.int64)
+        _vector(state, 2, "state")
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset must be in [0, 2^64)")
+    y = torch.empty_like(x) if out is None else out
+    rc = lib().nystra_dropout(_ptr(x), _ptr(residual), _ptr(y), x.numel(), p, seed, offset,
+                              _ptr(state), code, _raw_stream(x))
+    _check(rc, "nystra_dropout")
+    return y
+
+
+def _view(t):
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError("expected [windows, heads, tokens, width] with contiguous rows")
+    return View(t.data_ptr(), *t.stride()[:3])
+
+
+def _diff_shape(q, k, v, lam, kv_len, scale, causal):
+    import torch
+    for t in (q, k, v):
+        if t.dim() != 4:
+            raise ValueError("expected [windows, heads, tokens, width]")
+    _same(q, (k, v))
+    _same(q, (lam,), torch.float32)
+    W, H2, nq, d = q.shape
+    G, nk, dv = v.shape[1:]
+    if H2 % 2 != 0 or k.shape != (W, 2 * G, nk, d) or v.shape[0] != W:
+        raise ValueError("expected q [W, 2H, n_q, d], k [W, 2G, n_k, d] and v [W, G, n_k, d_v]")
+    _vector(lam, H2 // 2, "lam")
+    if kv_len is not None:
+        _same(q, (kv_len,), torch.int32)
+        _vector(kv_len, W, "kv_len")
+    return DiffShape(W, H2 // 2, G, nq, nk, d, dv, causal, scale)
+
+
+def nystra_diff_attn_workspace_size(shape, backward=False, dtype=F32):
+    n = ctypes.c_size_t(0)
+    _check(lib().nystra_diff_attn_workspace_size(ctypes.byref(shape), int(backward), dtype,
+                                                 ctypes.byref(n)),
+           "nystra_diff_attn_workspace_size")
+    return int(n.value)
+
+
+@_placed
+def nystra_diff_attn_forward(q, k, v, lam, scale=0.0, causal=CAUSAL_NONE, kv_len=None,
+                             with_saved=False, out=None, workspace=None):
+    """Differential attention, O = (softmax(s Q1 K1^T) - lam softmax(s Q2 K2^T)) V, of
+    q [W, 2H, n_q, d], k [W, 2G, n_k, d] and v [W, G, n_k, d_v] (heads 2h and 2h + 1 of q
+    and k are the two maps of head h; G divides H), lam fp32 [H]; any strides with
+    contiguous rows.  kv_len: int32 [W], the keys of each window; causal: CAUSAL_NONE,
+    CAUSAL_START or CAUSAL_END.  Returns O [W, H, n_q, d_v] or, with_saved, (O, saved):
+    what the backward pass needs besides the inputs."""
+    import torch
+    shape = _diff_shape(q, k, v, lam, kv_len, scale, causal)
+    code = _dtype_code(q)
+    oshape = (shape.n_windows, shape.heads, shape.n_q, shape.d_v)
+    if out is None:
+        out = torch.empty(oshape, dtype=q.dtype, device=q.device)
+    elif tuple(out.shape) != oshape:
+        raise ValueError(f"out must be {list(oshape)}")
+    _same(q, (out,))
+    o2 = lse = None
+    if with_saved:
+        lse = torch.empty((shape.n_windows, 2 * shape.heads, shape.n_q), dtype=torch.float32,
+                          device=q.device)
+        if shape.n_k > DIFF_SHORT_KEYS:
+            o2 = torch.empty(oshape, dtype=q.dtype, device=q.device)
+    if workspace is None:
+        need = nystra_diff_attn_workspace_size(shape, False, code)
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    else:
+        _same(q, (workspace,), workspace.dtype)
+    rc = lib().nystra_diff_attn_forward(_view(q), _view(k), _view(v), _ptr(lam), _ptr(kv_len),
+                                        _view(out), _ptr(o2), _ptr(lse), shape, code,
+                                        _ptr(workspace), _bytes(workspace), _raw_stream(q))
+    _check(rc, "nystra_diff_attn_forward")
+    return (out, (o2, lse)) if with_saved else out
+
+
+@_placed
+def nystra_diff_attn_backward(do, q, k, v, lam, o, saved, scale=0.0, causal=CAUSAL_NONE,
+                              kv_len=None, grads=None, workspace=None):
+    """(dq, dk, dv, dlam) of nystra_diff_attn_forward from its inputs, its output and
+    what it saved.  grads: (dq, dk, dv) to write into, strided like the inputs may be."""
+    import torch
+    shape = _diff_shape(q, k, v, lam, kv_len, scale, causal)
+    code = _dtype_code(q)
+    o2, lse = saved
+    oshape = (shape.n_windows, shape.heads, shape.n_q, shape.d_v)
+    if tuple(do.shape) != oshape or tuple(o.shape) != oshape:
+        raise ValueError(f"do and o must be {list(oshape)}")
+    _same(do, (q, o, o2))
+    _same(do, (lse,), torch.float32)
+    _vector(o2, o.numel(), "saved output")
+    _vector(lse, 2 * shape.n_windows * shape.heads * shape.n_q, "saved sums")
+    if grads is None:
+        grads = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dq, dk, dv = grads
+    for t, like in zip(grads, (q, k, v)):
+        if t.shape != like.shape:
+            raise ValueError("the gradients must have their inputs' shapes")
+    _same(do, grads)
+    dlam = torch.empty_like(lam)
+    if workspace is None:
+        need = nystra_diff_attn_workspace_size(shape, True, code)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    else:
+        _same(do, (workspace,), workspace.dtype)
+    rc = lib().nystra_diff_attn_backward(_view(do), _view(q), _view(k), _view(v), _ptr(lam),
+                                         _ptr(kv_len), _view(o), _ptr(o2), _ptr(lse), _view(dq),
+                                         _view(dk), _view(dv), _ptr(dlam), shape, code,
+                                         _ptr(workspace), _bytes(workspace), _raw_stream(q))
+    _check(rc, "nystra_diff_attn_backward")
+    return dq, dk, dv, dlam

@@ -797,6 +797,396 @@ int nystra_layer_forward(const void *X, const void *Wqkv, const void *bqkv, cons
                          dtype, opts, attention, workspace, workspace_bytes, stream, layer);
 }
 
+}  // extern "C"
+
+namespace {
+
+constexpr int kMaxNormChannels = 4096;
+
+struct Range {
+    const void *p;
+    int64_t bytes;
+};
+
+bool range_hits(const Range &a, const Range &b)
+{
+    return a.p && b.p && a.bytes > 0 && b.bytes > 0 && overlaps(a.p, a.bytes, b.p, b.bytes);
+}
+
+int check_norm(int64_t rows, int channels, int dtype)
+{
+    if (dtype != NYSTRA_F32 && dtype != NYSTRA_BF16)
+        return NYSTRA_ERR_DTYPE;
+    if (rows < 0 || rows >= (int64_t(1) << 31) || channels < 1 || channels > kMaxNormChannels)
+        return NYSTRA_ERR_SHAPE;
+    return NYSTRA_OK;
+}
+
+constexpr int64_t kMaxStride = int64_t(1) << 40;
+
+bool bad_stride(int64_t stride, int64_t least) { return stride < least || stride > kMaxStride; }
+
+int64_t rows_range(int64_t rows, int64_t stride, int channels, int eb)
+{
+    return rows > 0 ? ((rows - 1) * stride + channels) * eb : 0;
+}
+
+// The call of a differential-attention entry point without its tensors.
+int diff_problem(const nystra_diff_shape *s, int dtype, nystra::DiffProblem *p)
+{
+    if (!s)
+        return NYSTRA_ERR_NULL;
+    if (dtype != NYSTRA_F32 && dtype != NYSTRA_BF16)
+        return NYSTRA_ERR_DTYPE;
+    if (s->n_windows < 0 || s->kv_heads < 1 || s->heads < s->kv_heads ||
+        s->heads % s->kv_heads != 0 || s->n_q < 1 || s->n_q > kMaxN || s->n_k < 1 ||
+        s->n_k > kMaxN || s->d_qk < 1 || s->d_qk > 64 || s->d_v < 1 || s->d_v > 128 ||
+        int64_t(s->n_windows) * s->heads > kMaxUnits)
+        return NYSTRA_ERR_SHAPE;
+    if (s->causal < NYSTRA_CAUSAL_NONE || s->causal > NYSTRA_CAUSAL_END || !isfinite(s->scale))
+        return NYSTRA_ERR_ARG;
+    *p = nystra::DiffProblem{};
+    p->W = s->n_windows;
+    p->H = s->heads;
+    p->G = s->kv_heads;
+    p->R = s->heads / s->kv_heads;
+    p->nq = s->n_q;
+    p->nk = s->n_k;
+    p->d = s->d_qk;
+    p->dv = s->d_v;
+    p->causal = s->causal;
+    p->dtype = dtype;
+    p->scale = s->scale > 0.f ? s->scale : float(1.0 / sqrt(double(s->d_qk)));
+    p->scale2 = float(double(p->scale) * 1.4426950408889634);
+    return nystra::diff_grid_fits(*p) ? NYSTRA_OK : NYSTRA_ERR_SHAPE;
+}
+
+// One [windows][heads][tokens][width] view: present, aligned, strides in range, and
+// for an output no two elements in one place.
+int check_view(const nystra_view *v, int64_t windows, int64_t heads, int64_t tokens, int width,
+               int eb, bool output, nystra::DiffView *out, Range *range)
+{
+    if (!v || !v->data)
+        return NYSTRA_ERR_NULL;
+    if (misaligned(v->data, eb))
+        return NYSTRA_ERR_ALIGN;
+    const int64_t size[3] = {windows, heads, tokens};
+    int64_t stride[3] = {v->window, v->head, v->token};
+    int64_t last = width - 1;
+    for (int i = 0; i < 3; ++i) {
+        if (size[i] == 1)
+            stride[i] = 0;   // never stepped over, whatever the caller holds there
+        if (stride[i] < 0 || stride[i] > kMaxStride)
+            return NYSTRA_ERR_SHAPE;
+        last += (size[i] - 1) * stride[i];
+    }
+    if (output) {
+        // From the smallest stride up, each dimension steps past all of the ones below.
+        int64_t extent = width;
+        bool done[3] = {};
+        for (int n = 0; n < 3; ++n) {
+            int at = -1;
+            for (int i = 0; i < 3; ++i)
+                if (!done[i] && (at < 0 || size[i] == 1 ||
+                                 (size[at] != 1 && stride[i] < stride[at])))
+                    at = i;
+            done[at] = true;
+            if (size[at] == 1)
+                continue;
+            if (stride[at] < extent)
+                return NYSTRA_ERR_OVERLAP;
+            extent += (size[at] - 1) * stride[at];
+        }
+    }
+    *out = nystra::DiffView{v->data, stride[0], stride[1], stride[2]};
+    *range = Range{v->data, (last + 1) * eb};
+    return NYSTRA_OK;
+}
+
+int check_workspace(void *workspace, size_t bytes, size_t need, const Range *tensors, int n)
+{
+    if (need == 0)
+        return NYSTRA_OK;
+    if (!workspace || bytes < need || misaligned(workspace, 256))
+        return NYSTRA_ERR_WORKSPACE;
+    for (int i = 0; i < n; ++i)
+        if (range_hits(Range{workspace, int64_t(need)}, tensors[i]))
+            return NYSTRA_ERR_WORKSPACE;
+    return NYSTRA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int nystra_layer_norm_forward(const void *X, int64_t x_stride, const void *weight,
+                              const void *bias, void *Y, int64_t y_stride, float *mean,
+                              float *rstd, int64_t rows, int channels, float eps, int dtype,
+                              void *stream)
+{
+    const int rc = check_norm(rows, channels, dtype);
+    if (rc != NYSTRA_OK)
+        return rc;
+    if (!isfinite(eps) || eps < 0.f)
+        return NYSTRA_ERR_ARG;
+    if (rows == 0)
+        return NYSTRA_OK;
+    if (!X || !Y || !mean != !rstd)
+        return NYSTRA_ERR_NULL;
+    if (bad_stride(x_stride, channels) || bad_stride(y_stride, channels))
+        return NYSTRA_ERR_SHAPE;
+    const int eb = dtype_bytes(dtype);
+    if (misaligned(X, eb) || misaligned(Y, eb) || misaligned(weight, eb) || misaligned(bias, eb) ||
+        misaligned(mean, 4) || misaligned(rstd, 4))
+        return NYSTRA_ERR_ALIGN;
+    const Range in[] = {{X, rows_range(rows, x_stride, channels, eb)},
+                        {weight, int64_t(channels) * eb}, {bias, int64_t(channels) * eb}};
+    const Range out[] = {{Y, rows_range(rows, y_stride, channels, eb)}, {mean, rows * 4},
+                         {rstd, rows * 4}};
+    for (int i = 0; i < 3; ++i) {
+        for (const Range &r : in)
+            if (range_hits(out[i], r))
+                return NYSTRA_ERR_OVERLAP;
+        for (int j = 0; j < i; ++j)
+            if (range_hits(out[i], out[j]))
+                return NYSTRA_ERR_OVERLAP;
+    }
+    nystra::NormProblem p{};
+    p.x = X;
+    p.w = weight;
+    p.b = bias;
+    p.y = Y;
+    p.mean = mean;
+    p.rstd = rstd;
+    p.rows = rows;
+    p.x_stride = x_stride;
+    p.y_stride = y_stride;
+    p.C = channels;
+    p.dtype = dtype;
+    p.eps = eps;
+    clear_stale_error();
+    return finish_launch(nystra::launch_norm_forward(p, static_cast<hipStream_t>(stream)));
+}
+
+int nystra_layer_norm_workspace_size(int64_t rows, int channels, size_t *bytes)
+{
+    if (!bytes)
+        return NYSTRA_ERR_NULL;
+    const int rc = check_norm(rows, channels, NYSTRA_F32);
+    if (rc != NYSTRA_OK)
+        return rc;
+    *bytes = nystra::norm_workspace_bytes(rows, channels);
+    return NYSTRA_OK;
+}
+
+int nystra_layer_norm_backward(const void *dY, int64_t dy_stride, const void *X, int64_t x_stride,
+                               const void *weight, const float *mean, const float *rstd, void *dX,
+                               int64_t dx_stride, void *dweight, void *dbias, int64_t rows,
+                               int channels, int dtype, void *workspace, size_t workspace_bytes,
+                               void *stream)
+{
+    int rc = check_norm(rows, channels, dtype);
+    if (rc != NYSTRA_OK)
+        return rc;
+    if (rows > 0 && (!dY || !X || !mean || !rstd || !dX))
+        return NYSTRA_ERR_NULL;
+    if (rows > 0 && (bad_stride(dy_stride, channels) || bad_stride(x_stride, channels) ||
+                     bad_stride(dx_stride, channels)))
+        return NYSTRA_ERR_SHAPE;
+    const int eb = dtype_bytes(dtype);
+    for (const void *t : {dY, X, weight, static_cast<const void *>(dX),
+                          static_cast<const void *>(dweight), static_cast<const void *>(dbias)})
+        if (misaligned(t, eb))
+            return NYSTRA_ERR_ALIGN;
+    if (misaligned(mean, 4) || misaligned(rstd, 4))
+        return NYSTRA_ERR_ALIGN;
+    const int64_t cb = int64_t(channels) * eb;
+    const Range t[] = {{dX, rows_range(rows, dx_stride, channels, eb)}, {dweight, cb}, {dbias, cb},
+                       {dY, rows_range(rows, dy_stride, channels, eb)},
+                       {X, rows_range(rows, x_stride, channels, eb)}, {weight, cb},
+                       {mean, rows * 4}, {rstd, rows * 4}};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 8; ++j)
+            if (range_hits(t[i], t[j]))
+                return NYSTRA_ERR_OVERLAP;
+    rc = check_workspace(workspace, workspace_bytes, nystra::norm_workspace_bytes(rows, channels),
+                         t, 8);
+    if (rc != NYSTRA_OK)
+        return rc;
+    if (rows == 0 && !dweight && !dbias)
+        return NYSTRA_OK;
+    nystra::NormProblem p{};
+    p.x = X;
+    p.w = weight;
+    p.dy = dY;
+    p.dx = dX;
+    p.mean = const_cast<float *>(mean);
+    p.rstd = const_cast<float *>(rstd);
+    p.rows = rows;
+    p.x_stride = x_stride;
+    p.dy_stride = dy_stride;
+    p.dx_stride = dx_stride;
+    p.C = channels;
+    p.dtype = dtype;
+    clear_stale_error();
+    return finish_launch(nystra::launch_norm_backward(p, dweight, dbias,
+                                                      static_cast<float *>(workspace),
+                                                      static_cast<hipStream_t>(stream)));
+}
+
+int nystra_dropout(const void *X, const void *residual, void *Y, int64_t n, float p,
+                   uint64_t seed, uint64_t offset, const uint64_t *state, int dtype, void *stream)
+{
+    if (dtype != NYSTRA_F32 && dtype != NYSTRA_BF16)
+        return NYSTRA_ERR_DTYPE;
+    if (n < 0 || n > (int64_t(1) << 34))
+        return NYSTRA_ERR_SHAPE;
+    if (!(p >= 0.f && p <= 1.f))
+        return NYSTRA_ERR_ARG;
+    if (n == 0)
+        return NYSTRA_OK;
+    if (!X || !Y)
+        return NYSTRA_ERR_NULL;
+    const int eb = dtype_bytes(dtype);
+    if (misaligned(X, eb) || misaligned(residual, eb) || misaligned(Y, eb) || misaligned(state, 8))
+        return NYSTRA_ERR_ALIGN;
+    const Range y{Y, n * eb};
+    if ((X != Y && range_hits(y, Range{X, n * eb})) ||
+        (residual != Y && range_hits(y, Range{residual, n * eb})) ||
+        range_hits(y, Range{state, 16}))
+        return NYSTRA_ERR_OVERLAP;
+    nystra::DropProblem d;
+    d.x = X;
+    d.residual = residual;
+    d.y = Y;
+    d.n = n;
+    d.seed = seed;
+    d.offset = offset;
+    d.state = state;
+    d.threshold = uint32_t(floor(double(p) * 65536.0 + 0.5));
+    d.scale = d.threshold < 65536u ? float(65536.0 / (65536.0 - d.threshold)) : 0.f;
+    d.dtype = dtype;
+    clear_stale_error();
+    return finish_launch(nystra::launch_dropout(d, static_cast<hipStream_t>(stream)));
+}
+
+int nystra_diff_attn_workspace_size(const nystra_diff_shape *shape, int backward, int dtype,
+                                    size_t *bytes)
+{
+    if (!bytes)
+        return NYSTRA_ERR_NULL;
+    nystra::DiffProblem p;
+    const int rc = diff_problem(shape, dtype, &p);
+    if (rc != NYSTRA_OK)
+        return rc;
+    *bytes = p.W == 0    ? 0
+             : backward ? nystra::diff_backward_workspace(p)
+                        : nystra::diff_forward_workspace(p);
+    return NYSTRA_OK;
+}
+
+int nystra_diff_attn_forward(const nystra_view *Q, const nystra_view *K, const nystra_view *V,
+                             const float *lambda, const int32_t *kv_len, const nystra_view *O,
+                             void *O2, float *lse, const nystra_diff_shape *shape, int dtype,
+                             void *workspace, size_t workspace_bytes, void *stream)
+{
+    nystra::DiffProblem p;
+    int rc = diff_problem(shape, dtype, &p);
+    if (rc != NYSTRA_OK)
+        return rc;
+    if (p.W == 0)
+        return NYSTRA_OK;
+    const int eb = dtype_bytes(dtype);
+    Range t[8] = {};   // O, O2, lse, then the inputs
+    if ((rc = check_view(O, p.W, p.H, p.nq, p.dv, eb, true, &p.o, &t[0])) != NYSTRA_OK ||
+        (rc = check_view(Q, p.W, 2 * p.H, p.nq, p.d, eb, false, &p.q, &t[3])) != NYSTRA_OK ||
+        (rc = check_view(K, p.W, 2 * p.G, p.nk, p.d, eb, false, &p.k, &t[4])) != NYSTRA_OK ||
+        (rc = check_view(V, p.W, p.G, p.nk, p.dv, eb, false, &p.v, &t[5])) != NYSTRA_OK)
+        return rc;
+    if (!lambda)
+        return NYSTRA_ERR_NULL;
+    if (misaligned(O2, eb) || misaligned(lse, 4) || misaligned(lambda, 4) || misaligned(kv_len, 4))
+        return NYSTRA_ERR_ALIGN;
+    // The backward pass reads O2 for many keys and forms the same sums itself for few.
+    if ((O2 && !lse) || (lse && (O2 != nullptr) != (p.nk > NYSTRA_DIFF_SHORT_KEYS)))
+        return NYSTRA_ERR_NULL;
+    const int64_t rows = int64_t(p.W) * p.H * p.nq;
+    t[1] = Range{O2, rows * p.dv * eb};
+    t[2] = Range{lse, rows * 8};
+    t[6] = Range{lambda, int64_t(p.H) * 4};
+    t[7] = Range{kv_len, int64_t(p.W) * 4};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 8; ++j)
+            if (range_hits(t[i], t[j]))
+                return NYSTRA_ERR_OVERLAP;
+    rc = check_workspace(workspace, workspace_bytes, nystra::diff_forward_workspace(p), t, 8);
+    if (rc != NYSTRA_OK)
+        return rc;
+    p.o2 = O2;
+    p.lse = lse;
+    p.lambda = lambda;
+    p.kv_len = kv_len;
+    clear_stale_error();
+    return finish_launch(
+        nystra::launch_diff_forward(p, workspace, static_cast<hipStream_t>(stream)));
+}
+
+int nystra_diff_attn_backward(const nystra_view *dO, const nystra_view *Q, const nystra_view *K,
+                              const nystra_view *V, const float *lambda, const int32_t *kv_len,
+                              const nystra_view *O, const void *O2, const float *lse,
+                              const nystra_view *dQ, const nystra_view *dK, const nystra_view *dV,
+                              float *dlambda, const nystra_diff_shape *shape, int dtype,
+                              void *workspace, size_t workspace_bytes, void *stream)
+{
+    nystra::DiffProblem p;
+    int rc = diff_problem(shape, dtype, &p);
+    if (rc != NYSTRA_OK)
+        return rc;
+    if (!dlambda)
+        return NYSTRA_ERR_NULL;
+    if (misaligned(dlambda, 4))
+        return NYSTRA_ERR_ALIGN;
+    if (p.W > 0) {
+        const int eb = dtype_bytes(dtype);
+        const int64_t rows = int64_t(p.W) * p.H * p.nq;
+        Range t[13] = {};   // dQ, dK, dV, dlambda, then the inputs
+        if ((rc = check_view(dQ, p.W, 2 * p.H, p.nq, p.d, eb, true, &p.gq, &t[0])) != NYSTRA_OK ||
+            (rc = check_view(dK, p.W, 2 * p.G, p.nk, p.d, eb, true, &p.gk, &t[1])) != NYSTRA_OK ||
+            (rc = check_view(dV, p.W, p.G, p.nk, p.dv, eb, true, &p.gv, &t[2])) != NYSTRA_OK ||
+            (rc = check_view(dO, p.W, p.H, p.nq, p.dv, eb, false, &p.go, &t[4])) != NYSTRA_OK ||
+            (rc = check_view(Q, p.W, 2 * p.H, p.nq, p.d, eb, false, &p.q, &t[5])) != NYSTRA_OK ||
+            (rc = check_view(K, p.W, 2 * p.G, p.nk, p.d, eb, false, &p.k, &t[6])) != NYSTRA_OK ||
+            (rc = check_view(V, p.W, p.G, p.nk, p.dv, eb, false, &p.v, &t[7])) != NYSTRA_OK ||
+            (rc = check_view(O, p.W, p.H, p.nq, p.dv, eb, false, &p.o, &t[8])) != NYSTRA_OK)
+            return rc;
+        if (!lambda || !lse || (O2 != nullptr) != (p.nk > NYSTRA_DIFF_SHORT_KEYS))
+            return NYSTRA_ERR_NULL;
+        if (misaligned(O2, eb) || misaligned(lse, 4) || misaligned(lambda, 4) ||
+            misaligned(kv_len, 4))
+            return NYSTRA_ERR_ALIGN;
+        t[3] = Range{dlambda, int64_t(p.H) * 4};
+        t[9] = Range{O2, rows * p.dv * eb};
+        t[10] = Range{lse, rows * 8};
+        t[11] = Range{lambda, int64_t(p.H) * 4};
+        t[12] = Range{kv_len, int64_t(p.W) * 4};
+        for (int i = 0; i < 4; ++i)
+            for (int j = 3; j < 13; ++j)   // dQ, dK and dV may share a buffer
+                if (i != j && range_hits(t[i], t[j]))
+                    return NYSTRA_ERR_OVERLAP;
+        rc = check_workspace(workspace, workspace_bytes, nystra::diff_backward_workspace(p), t,
+                             13);
+        if (rc != NYSTRA_OK)
+            return rc;
+    }
+    p.o2 = const_cast<void *>(O2);
+    p.lse = const_cast<float *>(lse);
+    p.lambda = lambda;
+    p.kv_len = kv_len;
+    clear_stale_error();
+    return finish_launch(nystra::launch_diff_backward(p, workspace, dlambda,
+                                                      static_cast<hipStream_t>(stream)));
+}
+
 const char *nystra_status_str(int status)
 {
     switch (status) {

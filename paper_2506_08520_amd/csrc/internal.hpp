@@ -93,6 +93,69 @@ struct LayerTail {
 bool layer_supported(int64_t rows, int C, int heads, int dtype, int hidden);
 hipError_t launch_layer_tail(const LayerTail &t, hipStream_t stream);
 
+// LayerNorm over C channels of `rows` rows; strides in elements from row to row.
+// mean and rstd are written by the forward pass (may be null) and read by the
+// backward pass; w and b may be null (ones and zeros).
+struct NormProblem {
+    const void *x, *w, *b, *dy;
+    void *y, *dx;
+    float *mean, *rstd;
+    int64_t rows, x_stride, y_stride, dy_stride, dx_stride;
+    int C, dtype;
+    float eps;
+};
+hipError_t launch_norm_forward(const NormProblem &p, hipStream_t stream);
+// Column sums of the backward pass: workspace bytes, and the two launches.
+size_t norm_workspace_bytes(int64_t rows, int C);
+hipError_t launch_norm_backward(const NormProblem &p, void *dw, void *db, float *workspace,
+                                hipStream_t stream);
+
+// Dropout with an optional residual.  `threshold` of 65536 drops everything.
+// state (device, may be null): {seed, offset}, replaces seed and adds to offset.
+struct DropProblem {
+    const void *x, *residual;
+    void *y;
+    int64_t n;
+    uint64_t seed, offset;
+    const uint64_t *state;
+    uint32_t threshold;
+    float scale;
+    int dtype;
+};
+hipError_t launch_dropout(const DropProblem &p, hipStream_t stream);
+
+// A [window][head][token][width] tensor with strides in elements.
+struct DiffView {
+    void *data;
+    int64_t window, head, token;
+};
+
+// Differential attention.  The first part is the caller's, the second the
+// launcher's.
+struct DiffProblem {
+    DiffView q, k, v, o, go, gq, gk, gv;   // Q and K hold two heads per query / key head
+    void *o2;              // [W][H][nq][dv], the second map's output, or null
+    float *lse;            // [W][2H][nq], log2 of the sums of exponentials, or null
+    const float *lambda;   // [H]
+    const int32_t *kv_len; // [W] or null
+    int W, H, G, R;        // windows, query heads, key heads, H / G
+    int nq, nk, d, dv;
+    int causal;            // 0 none, 1 token i sees keys 0..i, 2 aligned at the last key
+    int dtype;
+    float scale, scale2;   // logit scale, and that times log2(e)
+
+    int vec_q, vec_k, vec_v, vec_go, vec_o, vec_o2;
+    bool vec_gq, vec_gk, vec_gv;
+    int tiles, ktiles, splits, chunk, dv4, partial_row;
+    float *partial, *rows_d1, *rows_d2, *rows_lam;
+};
+// Whether the grids of a call stay under the limits of a launch.
+bool diff_grid_fits(const DiffProblem &p);
+size_t diff_forward_workspace(const DiffProblem &p);
+size_t diff_backward_workspace(const DiffProblem &p);
+hipError_t launch_diff_forward(DiffProblem p, void *workspace, hipStream_t stream);
+hipError_t launch_diff_backward(DiffProblem p, void *workspace, float *glam, hipStream_t stream);
+
 // Head widths with a tiled instantiation: the multiples of 4 from 8 to 32
 // (Dehazeformer's 12 and 16, Uformer's 32) and SwinIR's 30.
 inline bool tiled_width(int d) { return d >= 8 && d <= 32 && (d % 4 == 0 || d == 30); }
