@@ -582,6 +582,12 @@ def nystra_diff_attn_workspace_size(shape, backward=False, dtype=F32):
     return int(n.value)
 
 
+def _kept(q, shape):
+    """What the backward pass needs of an output row: the second map's, and in bf16, whose
+    output is rounded, both."""
+    return (2, shape.d_v) if _dtype_code(q) == BF16 else (shape.d_v,)
+
+
 @_placed
 def nystra_diff_attn_forward(q, k, v, lam, scale=0.0, causal=CAUSAL_NONE, kv_len=None,
                              with_saved=False, out=None, workspace=None):
@@ -600,12 +606,12 @@ def nystra_diff_attn_forward(q, k, v, lam, scale=0.0, causal=CAUSAL_NONE, kv_len
     elif tuple(out.shape) != oshape:
         raise ValueError(f"out must be {list(oshape)}")
     _same(q, (out,))
-    o2 = lse = None
+    maps = lse = None
     if with_saved:
         lse = torch.empty((shape.n_windows, 2 * shape.heads, shape.n_q), dtype=torch.float32,
                           device=q.device)
         if shape.n_k > DIFF_SHORT_KEYS:
-            o2 = torch.empty(oshape, dtype=q.dtype, device=q.device)
+            maps = torch.empty(oshape[:3] + _kept(q, shape), dtype=torch.float32, device=q.device)
     if workspace is None:
         need = nystra_diff_attn_workspace_size(shape, False, code)
         if need > 0:
@@ -613,10 +619,10 @@ def nystra_diff_attn_forward(q, k, v, lam, scale=0.0, causal=CAUSAL_NONE, kv_len
     else:
         _same(q, (workspace,), workspace.dtype)
     rc = lib().nystra_diff_attn_forward(_view(q), _view(k), _view(v), _ptr(lam), _ptr(kv_len),
-                                        _view(out), _ptr(o2), _ptr(lse), shape, code,
+                                        _view(out), _ptr(maps), _ptr(lse), shape, code,
                                         _ptr(workspace), _bytes(workspace), _raw_stream(q))
     _check(rc, "nystra_diff_attn_forward")
-    return (out, (o2, lse)) if with_saved else out
+    return (out, (maps, lse)) if with_saved else out
 
 
 @_placed
@@ -627,13 +633,13 @@ def nystra_diff_attn_backward(do, q, k, v, lam, o, saved, scale=0.0, causal=CAUS
     import torch
     shape = _diff_shape(q, k, v, lam, kv_len, scale, causal)
     code = _dtype_code(q)
-    o2, lse = saved
+    maps, lse = saved
     oshape = (shape.n_windows, shape.heads, shape.n_q, shape.d_v)
     if tuple(do.shape) != oshape or tuple(o.shape) != oshape:
         raise ValueError(f"do and o must be {list(oshape)}")
-    _same(do, (q, o, o2))
-    _same(do, (lse,), torch.float32)
-    _vector(o2, o.numel(), "saved output")
+    _same(do, (q, o))
+    _same(do, (lse, maps), torch.float32)
+    _vector(maps, o.numel() * (2 if code == BF16 else 1), "saved maps")
     _vector(lse, 2 * shape.n_windows * shape.heads * shape.n_q, "saved sums")
     if grads is None:
         grads = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
@@ -649,7 +655,7 @@ def nystra_diff_attn_backward(do, q, k, v, lam, o, saved, scale=0.0, causal=CAUS
     else:
         _same(do, (workspace,), workspace.dtype)
     rc = lib().nystra_diff_attn_backward(_view(do), _view(q), _view(k), _view(v), _ptr(lam),
-                                         _ptr(kv_len), _view(o), _ptr(o2), _ptr(lse), _view(dq),
+                                         _ptr(kv_len), _view(o), _ptr(maps), _ptr(lse), _view(dq),
                                          _view(dk), _view(dv), _ptr(dlam), shape, code,
                                          _ptr(workspace), _bytes(workspace), _raw_stream(q))
     _check(rc, "nystra_diff_attn_backward")

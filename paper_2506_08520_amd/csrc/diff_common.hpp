@@ -1,0 +1,531 @@
+// Differential attention: the difference of two softmax maps over one set of
+// values, with a learned weight per head,
+//   S_a = s Q_a K_a^T (a = 1, 2),  P_a = softmax of S_a over the visible keys,
+//   O = (P_1 - lam P_2) V,
+// and its backward pass, with X = dO V^T and D_a = rowsum(P_a X):
+//   dS_1 = P_1 (X - D_1),  dS_2 = -lam P_2 (X - D_2),
+//   dQ_a = s dS_a K_a,  dK_a = s dS_a^T Q_a,  dV = (P_1 - lam P_2)^T dO,
+//   dlam = -sum over rows of D_2.
+//
+// A "unit" is a window and a key/value head; its rows are the queries of all R
+// query heads that share those keys, head after head (R n_q rows), so that a
+// single token of grouped heads still fills a tile.  One wave owns 32 rows (in
+// the dK, dV kernel 32 keys) and walks the other axis in tiles of 32 through
+// LDS.  Scores are formed transposed, S^T = K Q^T, so that a lane column is a
+// query: the running maximum and sum stay in the lane, and the probabilities
+// are the right-hand operand of O^T += V^T P^T as they stand.
+//
+// Fragments.  A 32 x 32 product over 16 contraction indices takes from lane
+// (g = lane / 32, c = lane % 32) eight values of row c of the left operand and
+// of column c of the right one, and returns D[8 (r / 4) + 4 g + r % 4][c] in
+// register r.  Which index a slot stands for is free as long as both operands
+// agree: operands read along rows (row_frag) use 8 g + j, those that meet a
+// product's result (col_frag) use that result's order, 8 (j / 4) + 4 g + j % 4.
+// bf16 runs it as one matrix instruction, fp32 as eight of depth two.
+#pragma once
+
+#include "device_common.hpp"
+#include "internal.hpp"
+
+namespace nystra {
+namespace diff {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+template <class E>
+struct Frag;
+
+template <>
+struct Frag<BF16> {
+    bf8 x;
+};
+
+template <>
+struct Frag<F32> {
+    float x[8];
+};
+
+__device__ inline f16v mma(const Frag<BF16> &a, const Frag<BF16> &b, f16v c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x, b.x, c, 0, 0, 0);
+}
+
+__device__ inline f16v mma(const Frag<F32> &a, const Frag<F32> &b, f16v c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[j], b.x[j], c, 0, 0, 0);
+    return c;
+}
+
+// Eight consecutive elements as they lie in memory.
+template <class E>
+struct alignas(16) Chunk {
+    uint32_t w[2 * E::bytes];
+};
+
+// Eight elements of a row from p, of which the row has n (n may be <= 0 or above 8); the
+// others, and all of them if the row is not `live`, are zero.  Every lane loads, from the
+// row's last elements where its own are not there, so that there are no branches.  WIDE:
+// rows are whole aligned 16-byte chunks; otherwise loads are of `vec` bytes (4 or the
+// element's for bf16, 16 or 4 for fp32), which divide the row's start and width.
+template <class E, bool WIDE>
+__device__ inline Chunk<E> load_chunk(const typename E::T *p, int n, bool live, int vec)
+{
+    Chunk<E> c;
+    if (E::bytes == 2 && WIDE) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(p + min(0, n - 8));
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            c.w[j] = live && n > 0 ? w[j] : 0u;
+    } else if (E::bytes == 4 && vec == 16) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(p + min(4 * h, n - 4));
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                c.w[4 * h + j] = live && 4 * h < n ? w[j] : 0u;
+        }
+    } else if (E::bytes == 4 || vec == 4) {
+        constexpr int per = 4 / E::bytes;
+#pragma unroll
+        for (int j = 0; j < 8 / per; ++j) {
+            const uint32_t u = *reinterpret_cast<const uint32_t *>(p + min(j * per, n - per));
+            c.w[j] = live && j * per < n ? u : 0u;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            uint32_t u = *reinterpret_cast<const uint16_t *>(p + min(j, n - 1));
+            u = live && j < n ? u : 0u;
+            c.w[j * E::bytes / 4] = j & 1 ? c.w[j * E::bytes / 4] | u << 16 : u;
+        }
+    }
+    return c;
+}
+
+template <class E>
+__device__ inline Frag<E> as_frag(const Chunk<E> &c)
+{
+    return __builtin_bit_cast(Frag<E>, c);
+}
+
+__device__ inline Frag<BF16> frag_of(const f16v &s, int c, BF16)
+{
+    typedef float f8 __attribute__((ext_vector_type(8)));
+    f8 v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        v[j] = s[8 * c + j];
+    return Frag<BF16>{__builtin_convertvector(v, bf8)};   // to nearest even
+}
+
+__device__ inline Frag<F32> frag_of(const f16v &s, int c, F32)
+{
+    Frag<F32> f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        f.x[j] = s[8 * c + j];
+    return f;
+}
+
+// A tile of rows of COLS elements in LDS, in chunks of eight elements.  Row fragments read
+// the same chunk of eight rows at a time, the transposing reads below two neighbouring
+// chunks of four rows; over the 64 banks of 4 bytes neither may meet a bank twice.  bf16
+// rows lie without gaps (so that loads can go to LDS directly) with their chunks exchanged
+// by a number from the row; fp32 rows, which have no transposing reads, are 16 bytes apart.
+template <class E, int COLS>
+struct Tile {
+    static constexpr int pitch = E::bytes == 2 ? COLS : COLS + 4;
+    static constexpr int kRow = COLS / 8;
+
+    __device__ static inline int swap(int row)
+    {
+        if constexpr (E::bytes == 4)
+            return 0;
+        else
+            return COLS == 32 ? (row >> 2) & 3 : COLS == 64 ? row & 7 : (row & 7) << 1;
+    }
+    __device__ static inline int at(int row, int chunk)
+    {
+        return row * pitch + 8 * (chunk ^ swap(row));
+    }
+};
+
+// Row lane % 32 of a tile, contraction indices (columns) 16 c + 8 g + j.
+template <class E, int COLS>
+__device__ inline Frag<E> row_frag(const typename E::T *tile, int c)
+{
+    const int lane = threadIdx.x & 63;
+    return as_frag<E>(*reinterpret_cast<const Chunk<E> *>(
+        tile + Tile<E, COLS>::at(lane & 31, 2 * c + (lane >> 5))));
+}
+
+// Column col0 + lane % 32 of a tile, contraction indices (rows) in the order of a
+// product's result: 16 c + 8 (j / 4) + 4 g + j % 4.  In bf16 the transposing LDS
+// read takes four rows of 16 columns from 16 lanes (lane p: row p / 4, columns
+// 4 (p % 4) ..) and gives each lane its column of them.
+template <class E, int COLS>
+__device__ inline Frag<E> col_frag(const typename E::T *tile, int c, int col0)
+{
+    using L = Tile<E, COLS>;
+    const int lane = threadIdx.x & 63, g = lane >> 5;
+    if constexpr (E::bytes == 2) {
+        typedef __attribute__((address_space(3))) s4 ls4;
+        const int row = 16 * c + 4 * g + ((lane & 15) >> 2);
+        const int col = col0 + (lane & 16) + 4 * (lane & 3);
+        struct {
+            s4 lo, hi;
+        } v;
+        v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (ls4 *)(tile + L::at(row, col >> 3) + (col & 7)));
+        v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (ls4 *)(tile + L::at(row + 8, col >> 3) + (col & 7)));
+        return __builtin_bit_cast(Frag<BF16>, v);
+    } else {
+        Frag<F32> f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            f.x[j] = tile[(16 * c + 8 * (j >> 2) + 4 * g + (j & 3)) * L::pitch + col0 +
+                          (lane & 31)];
+        return f;
+    }
+}
+
+// Walks a [rows][COLS] tile in chunks of eight elements over the NT threads of a
+// workgroup: loaded into registers while the tile before it is worked on, stored to LDS
+// when that is done.
+template <class E, int COLS, int ROWS, int NT>
+struct Stage {
+    using L = Tile<E, COLS>;
+    static constexpr int kAll = ROWS * L::kRow;
+    static constexpr int kN = (kAll + NT - 1) / NT;
+    Chunk<E> x[kN];
+
+    // at(row) points to the first element of a row, live(row) says whether it is there.
+    // Row 0 is always there.
+    template <class At, class Live>
+    __device__ inline void load(At at, Live live, int cols, int vec)
+    {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int id = threadIdx.x + i * NT;
+            const int row = id / L::kRow % ROWS, col = id % L::kRow * 8;
+            const bool in = live(row);
+            x[i] = load_chunk<E, false>(at(in ? row : 0) + col, cols - col, in, vec);
+        }
+    }
+
+    __device__ inline void store(typename E::T *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int id = threadIdx.x + i * NT;
+            if (kAll % NT == 0 || id < kAll)
+                *reinterpret_cast<Chunk<E> *>(lds + L::at(id / L::kRow, id % L::kRow)) = x[i];
+        }
+    }
+};
+
+// 16 bytes from `base` plus each lane's offset to LDS, lane after lane from `lds` on, past
+// the registers.  Nothing waits for it but arrived().  base and lds are the wave's.
+__device__ inline void load_to_lds(const void *base, uint32_t offset, void *lds)
+{
+    const uint32_t to = __builtin_amdgcn_readfirstlane(
+        uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void *)lds)));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(to), "v"(offset), "s"(base) : "memory");
+}
+
+__device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The same tile by loads that go to LDS directly, for rows of whole 16-byte chunks; at(row)
+// is the row's offset from `base` in elements, below 2^30.  Every lane loads: rows that are
+// not there must be given as another's (their products are masked), and columns from `cols`
+// on hold the last chunk again (the other operand is zero there).
+template <int COLS, int ROWS, int NT, class At>
+__device__ inline void direct_tile(uint16_t *lds, const void *base, At at, int cols)
+{
+    using L = Tile<BF16, COLS>;
+    static_assert(ROWS * L::kRow % NT == 0, "whole waves");
+#pragma unroll
+    for (int i = 0; i < ROWS * L::kRow / NT; ++i) {
+        const int id = threadIdx.x + i * NT;
+        const int row = id / L::kRow, chunk = id % L::kRow ^ L::swap(row);
+        const int col = min(8 * chunk, cols - 8);
+        load_to_lds(base, 2 * uint32_t(at(row) + col), lds + (i * NT + (threadIdx.x & ~63u)) * 8);
+    }
+}
+
+__device__ inline float other_half(float x)
+{
+    return __shfl_xor(x, 32, 64);
+}
+
+// r / n_q for 0 <= r < 2^30: with k = 31 + floor(log2 n_q) and M = ceil(2^k / n_q), M n_q
+// exceeds 2^k by less than n_q < 2^(k - 30), so floor(r M / 2^k) is exact.
+__device__ inline int div_nq(const DiffProblem &p, int r)
+{
+    return int((uint64_t(uint32_t(r)) * p.nq_mul) >> p.nq_shift);
+}
+
+// Position of a row of the unit: its query head and token.
+struct Row {
+    int head, token;
+};
+
+__device__ inline Row row_of(const DiffProblem &p, int g, int r)
+{
+    const int hh = div_nq(p, r);
+    return Row{g * p.R + hh, r - hh * p.nq};
+}
+
+// Keys that a query token sees: those below the returned index.
+__device__ inline int key_limit(const DiffProblem &p, int len, int token)
+{
+    if (p.causal == 0)
+        return len;
+    const int n = p.causal == 1 ? token + 1 : len - p.nq + token + 1;
+    return n < 0 ? 0 : n < len ? n : len;
+}
+
+__device__ inline int window_len(const DiffProblem &p, int w)
+{
+    if (!p.kv_len)
+        return p.nk;
+    const int n = p.kv_len[w];
+    return n < 0 ? 0 : n < p.nk ? n : p.nk;
+}
+
+// Keys that the rows r0 .. r1 see at most: the limit grows with the token, and
+// rows of several heads hold the last token of the first one.
+__device__ inline int tile_limit(const DiffProblem &p, int len, int r0, int r1)
+{
+    const int h1 = div_nq(p, r1);
+    if (div_nq(p, r0) != h1)
+        return key_limit(p, len, p.nq - 1);
+    return key_limit(p, len, r1 - h1 * p.nq);
+}
+
+template <class E>
+__device__ inline const typename E::T *at(const DiffView &v, int64_t w, int64_t head, int64_t token)
+{
+    return static_cast<const typename E::T *>(v.data) + w * v.window + head * v.head +
+           token * v.token;
+}
+
+template <class E>
+__device__ inline typename E::T *at_out(const DiffView &v, int64_t w, int64_t head, int64_t token)
+{
+    return static_cast<typename E::T *>(v.data) + w * v.window + head * v.head + token * v.token;
+}
+
+// Four consecutive elements of an output row from column `col`, those below `n`; `vec`
+// says that such groups are whole and aligned.
+template <class E>
+__device__ inline void store4(typename E::T *row, int col, int n, bool vec, float a, float b,
+                              float c, float d)
+{
+    if (vec) {
+        if (col < n) {
+            if constexpr (E::bytes == 4) {
+                *reinterpret_cast<float4 *>(row + col) = make_float4(a, b, c, d);
+            } else {
+                typedef float f4 __attribute__((ext_vector_type(4)));
+                typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<b4 *>(row + col) = __builtin_convertvector((f4{a, b, c, d}), b4);
+            }
+        }
+        return;
+    }
+    const float x[4] = {a, b, c, d};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (col + j < n) {
+            if constexpr (E::bytes == 4)
+                row[col + j] = x[j];
+            else
+                reinterpret_cast<__bf16 *>(row)[col + j] = __bf16(x[j]);
+        }
+}
+
+// What is kept of a row for the backward pass, in fp32: the second map's output, and
+// where O itself is rounded to bf16 the first one's, in [W][H][n_q][1 or 2][d_v].
+template <class E>
+__device__ inline float *map_row(const DiffProblem &p, int w, const Row &row)
+{
+    return p.maps + ((int64_t(w) * p.H + row.head) * p.nq + row.token) *
+                        (E::bytes == 2 ? 2 * p.dv : p.dv);
+}
+
+// The transposed tile's register r: its row.
+__device__ inline int reg_row(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
+
+// Scores of keys that a row does not see, in a tile of S^T.
+__device__ inline void hide(f16v &s, int limit, int k0, int g)
+{
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        s[r] = k0 + reg_row(r, g) < limit ? s[r] : -INFINITY;
+}
+
+// Online softmax of a 32 x 32 tile of S^T: s becomes exp2(scale2 s - m) and l the running
+// sum of this lane's keys.  m, the exponents' base, follows the running maximum only when
+// some row's has outgrown it by 2^8 (fp32 sums and bf16 terms keep their relative precision
+// below that), and `grow(alpha)` then rescales what was summed: with every new maximum
+// that would be in nearly every tile.
+template <class Grow>
+__device__ inline void softmax_step(f16v &s, float scale2, float &m, float &l, Grow grow)
+{
+    float t = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r)
+        t = fmaxf(t, s[r]);
+    t = fmaxf(t, other_half(t)) * scale2;
+    if (__any(t > m + 8.f)) {
+        const float mn = fmaxf(m, t);
+        // A row that has seen no key yet has nothing to rescale.
+        const float alpha = mn == -INFINITY ? 1.f : fast_exp2(m - mn);
+        l *= alpha;
+        m = mn;
+        grow(alpha);
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        s[r] = fast_exp2(fmaf(s[r], scale2, -base));
+        sum += s[r];
+    }
+    l += sum;
+}
+
+// Blocks of one unit run on one XCD (blocks go to the eight of them in turn), so
+// that the unit's keys and values are fetched into one L2 only.
+__device__ inline int64_t xcd_order(int64_t b, int64_t n)
+{
+    const int64_t per = n / 8, full = per * 8;
+    return b < full ? (b % 8) * per + b / 8 : b;
+}
+
+// Keys and values of a unit, tile after tile of KT keys, into two LDS buffers in turn:
+// fetch() starts on a tile, commit() ends it after the work on the one before, and ready()
+// is the barrier behind which it may be read.
+template <class E, int DK, int DV, int NT, bool DIRECT>
+struct KeyTiles {
+    static constexpr int KT = 32;
+    using T = typename E::T;
+    using LK = Tile<E, DK>;
+    using LV = Tile<E, DV>;
+    struct Buffer {
+        alignas(16) T k[2][KT * LK::pitch];
+        alignas(16) T v[KT * LV::pitch];
+    };
+    Stage<E, DK, 2 * KT, NT> k;   // both maps, one under the other
+    Stage<E, DV, KT, NT> v;
+
+    __device__ inline void fetch(const DiffProblem &p, const T *k0, const T *v0, int key, int end,
+                                 Buffer &to)
+    {
+        const int last = end - key - 1;
+        k0 += key * p.k.token;
+        v0 += key * p.v.token;
+        if constexpr (DIRECT) {
+            const int kh = int(p.k.head), kt = int(p.k.token), vt = int(p.v.token);
+            direct_tile<DK, 2 * KT, NT>(
+                to.k[0], k0, [&](int row) { return (row / KT) * kh + min(row % KT, last) * kt; },
+                p.d);
+            direct_tile<DV, KT, NT>(to.v, v0, [&](int row) { return min(row, last) * vt; }, p.dv);
+        } else {
+            k.load([&](int row) { return k0 + (row / KT) * p.k.head + (row % KT) * p.k.token; },
+                   [&](int row) { return row % KT <= last; }, p.d, p.vec_k);
+            v.load([&](int row) { return v0 + row * p.v.token; },
+                   [&](int row) { return row <= last; }, p.dv, p.vec_v);
+        }
+    }
+
+    __device__ inline void commit(Buffer &to) const
+    {
+        if constexpr (!DIRECT) {
+            k.store(to.k[0]);
+            v.store(to.v);
+        }
+    }
+
+    __device__ static inline void ready()
+    {
+        if constexpr (DIRECT)
+            arrived();
+        __syncthreads();
+    }
+};
+
+// Nothing is scheduled across: without it the operands of several products are fetched
+// ahead of the first, which takes more registers than two waves to a SIMD leave.
+__device__ inline void part() { __builtin_amdgcn_sched_barrier(0); }
+
+// Waves to a SIMD that the kernels are compiled for: two, whose matrix instructions and
+// exponentials run beside each other, except at full width for fp32 and for kernels with `more`
+// to hold, whose operands do not fit 256 registers.
+template <class E, int DV>
+constexpr int occupancy(bool more = false)
+{
+    return DV == 128 && (E::bytes == 4 || more) ? 1 : 2;
+}
+
+// ---- host side ----------------------------------------------------------------
+
+// Whether every row of a tensor starts and ends on a multiple of `to` bytes.
+inline bool aligned(const DiffView &v, int width, int bytes, int to)
+{
+    return uintptr_t(v.data) % to == 0 &&
+           (v.window | v.head | v.token | width) * bytes % to == 0;
+}
+
+// Bytes of one load where rows are not whole 16-byte chunks of bf16 (see load_chunk).
+inline int view_vec(const DiffView &v, int width, int bytes)
+{
+    if (bytes == 4)
+        return aligned(v, width, 4, 16) ? 16 : 4;
+    return aligned(v, width, 2, 4) ? 4 : 2;
+}
+
+// Whether tiles can be loaded to LDS directly: bf16 rows of whole 16-byte chunks, and
+// `span` elements, those of a tile or of a unit, within 32-bit offsets.
+inline bool direct(const DiffProblem &p, const DiffView &v, int width, int64_t span)
+{
+    return p.dtype == 1 && aligned(v, width, 2, 16) && span < (int64_t(1) << 30);
+}
+
+// Whether groups of four elements may be stored at once.
+inline bool store_vec(const DiffView &v, int width, int bytes)
+{
+    return uintptr_t(v.data) % (4 * bytes) == 0 && ((v.window | v.head | v.token | width) % 4) == 0;
+}
+
+inline int ceil_div(int64_t a, int64_t b) { return int((a + b - 1) / b); }
+
+inline int round4(int n) { return (n + 3) / 4 * 4; }
+
+// Waves to a workgroup: as many as there are tiles of 32 rows (or keys), at most four.
+inline int waves_for(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+
+// Widths are padded to 32 (queries, keys) and 64 (values) or to 64 and 128.
+inline bool narrow(const DiffProblem &p) { return p.d <= 32 && p.dv <= 64; }
+
+inline void set_common(DiffProblem *p)
+{
+    const int e = p->dtype == 0 ? 4 : 2;
+    p->vec_q = view_vec(p->q, p->d, e);
+    p->vec_k = view_vec(p->k, p->d, e);
+    p->vec_v = view_vec(p->v, p->dv, e);
+    p->nq_shift = 31 + (31 - __builtin_clz(unsigned(p->nq)));
+    p->nq_mul = uint32_t(((uint64_t(1) << p->nq_shift) + p->nq - 1) / p->nq);
+}
+
+}  // namespace diff
+}  // namespace nystra

@@ -1,0 +1,434 @@
+// Backward pass of differential attention, second half: dK, dV and dlam, key by key, and
+// the calls of both halves (the formulas stand in diff_common.hpp).
+#include <type_traits>
+
+#include "diff_common.hpp"
+
+namespace nystra {
+
+// The first half; p.row_stats and p.rows_lam are its results besides dQ.
+hipError_t launch_diff_dq(const DiffProblem &p, int waves, int64_t blocks, hipStream_t s);
+
+namespace {
+
+using namespace diff;
+
+constexpr int kMerge = 64;   // threads of the merge kernel: one key
+
+// dlam of one head: the sum over its rows in all windows, by one workgroup.
+template <int NT>
+__device__ inline void sum_dlam(const DiffProblem &p, int h, float *out)
+{
+    __shared__ float lds[NT / 64];
+    float s = 0.f;
+    const int n = p.W * p.nq;   // below 2^24
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const int w = div_nq(p, i);
+        s += p.rows_lam[(int64_t(w) * p.H + h) * p.nq + (i - w * p.nq)];
+    }
+    s = wave_sum(s);
+    if ((threadIdx.x & 63) == 0)
+        lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.f;
+        for (int i = 0; i < NT / 64; ++i)
+            s += lds[i];
+        out[h] = -s;
+    }
+}
+
+// dK and dV: a wave owns 32 keys and walks over the unit's rows, so that the heads
+// that share the keys are summed in registers.  Keys at or behind the window's
+// length get zeros.  With few workgroups the rows are split over p.rsplits of them, whose
+// sums go to the workspace.  The last H workgroups add up dlam meanwhile.
+template <class E, int DK, int DV, int NW, bool DIRECT>
+__global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>()))
+diff_dkv_kernel(DiffProblem p)
+{
+    using T = typename E::T;
+    constexpr int QT = 32, NT = 64 * NW;
+    using LQ = Tile<E, DK>;
+    using LG = Tile<E, DV>;
+    // The values' fragments stay in registers unless that halves the occupancy.
+    constexpr bool kLdsV = E::bytes == 2 && DV == 128;
+    struct Buffer {
+        alignas(16) T q[2][QT * LQ::pitch];
+        alignas(16) T go[QT * LG::pitch];
+        float4 stat[QT];                  // L_1, L_2, D_1, D_2
+        alignas(16) float lam[QT];
+        alignas(16) int lim[QT];
+    };
+    __shared__ Buffer buf[2];
+    __shared__ alignas(16) T vs[kLdsV ? NW * 32 * LG::pitch : 8];
+    const int64_t blocks = int64_t(gridDim.x) - p.H;
+    if (int64_t(blockIdx.x) >= blocks) {
+        sum_dlam<NT>(p, int(blockIdx.x - blocks), p.glam);
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
+    int64_t b = xcd_order(blockIdx.x, blocks);
+    const int split = int(b % p.rsplits);
+    b /= p.rsplits;
+    const int tile = int(b % p.ktiles);
+    const int64_t unit = b / p.ktiles;
+    const int w = int(unit / p.G), kvh = int(unit % p.G);
+    const int nrows = p.R * p.nq;
+    const int kb = tile * 32 * NW, kw = kb + wave * 32, key = kw + c;
+    const int len = window_len(p, w);
+    const bool live = key < len;
+
+    Frag<E> k[2][DK / 16], v[kLdsV ? 1 : DV / 16];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        const T *src = at<E>(p.k, w, 2 * kvh + a, live ? key : 0);
+#pragma unroll
+        for (int i = 0; i < DK / 16; ++i)
+            k[a][i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
+                                                       p.d - 16 * i - 8 * g, live, p.vec_k));
+    }
+    if constexpr (kLdsV) {
+        const T *v0 = at<E>(p.v, w, kvh, 0);
+        constexpr int kChunks = NW * 32 * LG::kRow / NT;
+#pragma unroll 4
+        for (int i = 0; i < kChunks; ++i) {
+            const int id = threadIdx.x + i * NT, row = id / LG::kRow, ch = id % LG::kRow;
+            const bool in = kb + row < len;
+            *reinterpret_cast<Chunk<E> *>(vs + LG::at(row, ch)) = load_chunk<E, DIRECT>(
+                v0 + (in ? kb + row : 0) * p.v.token + 8 * ch, p.dv - 8 * ch, in, p.vec_v);
+        }
+    } else {
+        const T *src = at<E>(p.v, w, kvh, live ? key : 0);
+#pragma unroll
+        for (int i = 0; i < DV / 16; ++i)
+            v[i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
+                                                    live, p.vec_v));
+    }
+    f16v gk[2][DK / 32] = {}, gv[DV / 32] = {};
+
+    Stage<E, DK, 2 * QT, NT> sq;
+    Stage<E, DV, QT, NT> sgo;
+    float4 sstat;
+    float slam;
+    // Tiles of rows from `from` on, past those that see no key of this workgroup.
+    const int rend = min(nrows, (split + 1) * p.rchunk);
+    auto next = [&](int from) {
+        while (from < rend && tile_limit(p, len, from, min(from + QT, nrows) - 1) <= kb)
+            from += QT;
+        return from;
+    };
+    using Off = std::conditional_t<DIRECT, int, int64_t>;
+    // A row's place from the unit's first: the heads that share the keys lie behind each
+    // other, head after head.
+    const T *q0 = at<E>(p.q, w, 2 * kvh * p.R, 0), *go0 = at<E>(p.go, w, kvh * p.R, 0);
+    auto q_row = [&](int r, int a) {
+        const Row row = row_of(p, 0, min(r, nrows - 1));
+        return (2 * row.head + a) * Off(p.q.head) + row.token * Off(p.q.token);
+    };
+    auto go_row = [&](int r) {
+        const Row row = row_of(p, 0, min(r, nrows - 1));
+        return row.head * Off(p.go.head) + row.token * Off(p.go.token);
+    };
+    auto fetch = [&](int r0, Buffer &t) {
+        if constexpr (DIRECT) {
+            direct_tile<DK, 2 * QT, NT>(
+                t.q[0], q0, [&](int i) { return q_row(r0 + i % QT, i / QT); }, p.d);
+            direct_tile<DV, QT, NT>(t.go, go0, [&](int i) { return go_row(r0 + i); }, p.dv);
+        } else {
+            sq.load([&](int i) { return q0 + q_row(r0 + i % QT, i / QT); },
+                    [&](int i) { return r0 + i % QT < nrows; }, p.d, p.vec_q);
+            sgo.load([&](int i) { return go0 + go_row(r0 + i); },
+                     [&](int i) { return r0 + i < nrows; }, p.dv, p.vec_go);
+        }
+        if (threadIdx.x < QT) {
+            sstat = p.row_stats[unit * p.rows32 + r0 + threadIdx.x];
+            slam = p.lambda[row_of(p, kvh, min(r0 + int(threadIdx.x), nrows - 1)).head];
+        }
+    };
+    auto commit = [&](int r0, Buffer &t) {
+        if constexpr (!DIRECT) {
+            sq.store(t.q[0]);
+            sgo.store(t.go);
+        }
+        if (threadIdx.x < QT) {
+            const int r = r0 + threadIdx.x;
+            t.stat[threadIdx.x] = sstat;
+            t.lam[threadIdx.x] = slam;
+            t.lim[threadIdx.x] =
+                r < nrows ? key_limit(p, len, row_of(p, kvh, r).token) : 0;
+        }
+    };
+    int r0 = kb < len ? next(split * p.rchunk) : rend;
+    if (r0 < rend) {
+        fetch(r0, buf[0]);
+        commit(r0, buf[0]);
+    }
+    for (int at_buf = 0; r0 < rend; at_buf ^= 1) {
+        if constexpr (DIRECT)
+            arrived();
+        __syncthreads();
+        const int r1 = next(r0 + QT);
+        if (r1 < rend)
+            fetch(r1, buf[at_buf ^ 1]);
+        const Buffer &t = buf[at_buf];
+        const int rowlim = t.lim[c];
+        if (__any(kw < rowlim)) {
+            const bool masked = !__all(kw + 32 <= rowlim);
+            f16v s[2] = {}, x = {};
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+#pragma unroll
+                for (int i = 0; i < DK / 16; ++i)
+                    s[a] = mma(row_frag<E, DK>(t.q[a], i), k[a][i], s[a]);
+                part();
+            }
+#pragma unroll
+            for (int i = 0; i < DV / 16; ++i) {
+                if constexpr (kLdsV)
+                    x = mma(row_frag<E, DV>(t.go, i),
+                            row_frag<E, DV>(vs + wave * 32 * LG::pitch, i), x);
+                else
+                    x = mma(row_frag<E, DV>(t.go, i), v[i], x);
+            }
+            part();
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const bool see = key < t.lim[reg_row(i, g)];
+                    s[0][i] = see ? s[0][i] : -INFINITY;
+                    s[1][i] = see ? s[1][i] : -INFINITY;
+                }
+            }
+            f16v pd;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 lm = *reinterpret_cast<const float4 *>(t.lam + 8 * j + 4 * g);
+                const float lam[4] = {lm.x, lm.y, lm.z, lm.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 4 * j + e;
+                    const float4 st = t.stat[reg_row(i, g)];
+                    const float p1 = fast_exp2(fmaf(s[0][i], p.scale2, -st.x));
+                    const float p2 = lam[e] * fast_exp2(fmaf(s[1][i], p.scale2, -st.y));
+                    pd[i] = p1 - p2;
+                    s[0][i] = p1 * (x[i] - st.z);
+                    s[1][i] = p2 * (st.w - x[i]);
+                }
+            }
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const bool one = t.lim[reg_row(i, g)] == 1;   // as in the dQ kernel
+                    s[0][i] = one ? 0.f : s[0][i];
+                    s[1][i] = one ? 0.f : s[1][i];
+                }
+            }
+            part();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const Frag<E> f = frag_of(pd, h, E());
+#pragma unroll
+                for (int i = 0; i < DV / 32; ++i)
+                    gv[i] = mma(col_frag<E, DV>(t.go, h, 32 * i), f, gv[i]);
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    const Frag<E> ds = frag_of(s[a], h, E());
+#pragma unroll
+                    for (int i = 0; i < DK / 32; ++i)
+                        gk[a][i] = mma(col_frag<E, DK>(t.q[a], h, 32 * i), ds, gk[a][i]);
+                }
+            }
+        }
+        if (r1 < rend)
+            commit(r1, buf[at_buf ^ 1]);
+        r0 = r1;
+    }
+    if (key >= p.nk)
+        return;
+    if (p.rsplits > 1) {
+        float *out = p.partial + ((unit * p.rsplits + split) * p.nk + key) * p.partial_row;
+#pragma unroll
+        for (int i = 0; i < DK / 32; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+                    store4<F32>(out + a * p.d4, 32 * i + 8 * j + 4 * g, p.d4, true,
+                                gk[a][i][4 * j], gk[a][i][4 * j + 1], gk[a][i][4 * j + 2],
+                                gk[a][i][4 * j + 3]);
+#pragma unroll
+        for (int i = 0; i < DV / 32; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                store4<F32>(out + 2 * p.d4, 32 * i + 8 * j + 4 * g, p.dv4, true, gv[i][4 * j],
+                            gv[i][4 * j + 1], gv[i][4 * j + 2], gv[i][4 * j + 3]);
+        return;
+    }
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        T *dst = at_out<E>(p.gk, w, 2 * kvh + a, key);
+#pragma unroll
+        for (int i = 0; i < DK / 32; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                store4<E>(dst, 32 * i + 8 * j + 4 * g, p.d, p.vec_gk,
+                          live ? p.scale * gk[a][i][4 * j] : 0.f,
+                          live ? p.scale * gk[a][i][4 * j + 1] : 0.f,
+                          live ? p.scale * gk[a][i][4 * j + 2] : 0.f,
+                          live ? p.scale * gk[a][i][4 * j + 3] : 0.f);
+    }
+    T *dst = at_out<E>(p.gv, w, kvh, key);
+#pragma unroll
+    for (int i = 0; i < DV / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            store4<E>(dst, 32 * i + 8 * j + 4 * g, p.dv, p.vec_gv, live ? gv[i][4 * j] : 0.f,
+                      live ? gv[i][4 * j + 1] : 0.f, live ? gv[i][4 * j + 2] : 0.f,
+                      live ? gv[i][4 * j + 3] : 0.f);
+}
+
+// Adds up the row ranges of one key.
+template <class E>
+__global__ void __launch_bounds__(kMerge)
+diff_dkv_merge_kernel(DiffProblem p)
+{
+    const int64_t unit = blockIdx.x / unsigned(p.nk);
+    const int key = int(blockIdx.x - unit * p.nk);
+    const int w = int(unit / p.G), kvh = int(unit % p.G);
+    const bool live = key < window_len(p, w);
+    const float *part = p.partial + (unit * p.rsplits * p.nk + key) * p.partial_row;
+    const int64_t step = int64_t(p.nk) * p.partial_row;
+    for (int col = threadIdx.x; col < 2 * p.d4 + p.dv4; col += kMerge) {
+        float s = 0.f;
+        if (live)
+            for (int i = 0; i < p.rsplits; ++i)
+                s += part[i * step + col];
+        if (col < 2 * p.d4) {
+            const int a = col >= p.d4, at_col = col - a * p.d4;
+            if (at_col < p.d)
+                E::store(at_out<E>(p.gk, w, 2 * kvh + a, key), at_col, p.scale * s);
+        } else if (col - 2 * p.d4 < p.dv) {
+            E::store(at_out<E>(p.gv, w, kvh, key), col - 2 * p.d4, s);
+        }
+    }
+}
+
+// No windows: the sum over nothing.
+__global__ void diff_dlam_zero_kernel(int n, float *glam)
+{
+    for (int i = threadIdx.x; i < n; i += blockDim.x)
+        glam[i] = 0.f;
+}
+
+// ---- dispatch -----------------------------------------------------------------
+
+template <class E, int DK, int DV, int NW>
+void run(const DiffProblem &p, int64_t blocks, hipStream_t s)
+{
+    const dim3 grid(unsigned(blocks + p.H));
+    if constexpr (E::bytes == 2) {
+        if (direct(p, p.k, p.d, 0) && direct(p, p.v, p.dv, 0) &&
+            direct(p, p.q, p.d, 2 * p.R * p.q.head + p.nq * p.q.token) &&
+            direct(p, p.go, p.dv, p.R * p.go.head + p.nq * p.go.token)) {
+            diff_dkv_kernel<E, DK, DV, NW, true><<<grid, 64 * NW, 0, s>>>(p);
+            return;
+        }
+    }
+    diff_dkv_kernel<E, DK, DV, NW, false><<<grid, 64 * NW, 0, s>>>(p);
+}
+
+template <class E>
+void run_any(const DiffProblem &p, int waves, int64_t blocks, hipStream_t s)
+{
+    if (waves == 2)
+        narrow(p) ? run<E, 32, 64, 2>(p, blocks, s) : run<E, 64, 128, 2>(p, blocks, s);
+    else
+        narrow(p) ? run<E, 32, 64, 4>(p, blocks, s) : run<E, 64, 128, 4>(p, blocks, s);
+}
+
+// Waves to a workgroup: two for up to 64 rows or keys, otherwise four.
+int backward_waves(int64_t n) { return n <= 64 ? 2 : 4; }
+
+int64_t round256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Row ranges of the dK, dV kernel: enough workgroups for the 256 CUs twice over, of at
+// least four tiles each.
+void plan_rows(DiffProblem *p, int waves)
+{
+    const int64_t rows = int64_t(p->R) * p->nq, units = int64_t(p->W) * p->G;
+    p->rows32 = int64_t(ceil_div(rows, 32)) * 32;
+    p->ktiles = ceil_div(p->nk, 32 * waves);
+    const int64_t blocks = units * p->ktiles;
+    const int most = ceil_div(rows, 128);
+    const int64_t want = blocks > 0 ? (512 + blocks - 1) / blocks : 1;
+    p->rsplits = int(want < most ? want : most);
+    p->rchunk = ceil_div(ceil_div(rows, p->rsplits), 32) * 32;
+    p->rsplits = ceil_div(rows, p->rchunk);
+    p->d4 = round4(p->d);
+    p->dv4 = round4(p->dv);
+    p->partial_row = 2 * p->d4 + p->dv4;
+}
+
+// The workspace's parts: a record of each row, dlam's rows, and dK and dV by row range.
+struct Parts {
+    int64_t stats, lam, partial;
+};
+
+Parts parts_of(const DiffProblem &p)
+{
+    const int64_t units = int64_t(p.W) * p.G;
+    return Parts{round256(units * p.rows32 * 16), round256(int64_t(p.W) * p.H * p.nq * 4),
+                 p.rsplits > 1 ? units * p.rsplits * p.nk * p.partial_row * 4 : 0};
+}
+
+}  // namespace
+
+size_t diff_backward_workspace(const DiffProblem &p)
+{
+    DiffProblem t = p;
+    plan_rows(&t, backward_waves(p.nk));
+    const Parts b = parts_of(t);
+    return size_t(b.stats + b.lam + b.partial);
+}
+
+hipError_t launch_diff_backward(DiffProblem p, void *workspace, hipStream_t s)
+{
+    const int e = p.dtype == 0 ? 4 : 2;
+    if (p.W == 0) {
+        diff_dlam_zero_kernel<<<1, 256, 0, s>>>(p.H, p.glam);
+        return hipGetLastError();
+    }
+    set_common(&p);
+    p.vec_go = view_vec(p.go, p.dv, e);
+    p.vec_o = view_vec(p.o, p.dv, e);
+    p.vec_gq = store_vec(p.gq, p.d, e);
+    p.vec_gk = store_vec(p.gk, p.d, e);
+    p.vec_gv = store_vec(p.gv, p.dv, e);
+    const int64_t rows = int64_t(p.R) * p.nq, units = int64_t(p.W) * p.G;
+    const int wq = backward_waves(rows), wk = backward_waves(p.nk);
+    p.tiles = ceil_div(rows, 32 * wq);
+    plan_rows(&p, wk);
+    const Parts b = parts_of(p);
+    char *ws = static_cast<char *>(workspace);
+    p.row_stats = reinterpret_cast<float4 *>(ws);
+    p.rows_lam = reinterpret_cast<float *>(ws + b.stats);
+    p.partial = reinterpret_cast<float *>(ws + b.stats + b.lam);
+    hipError_t err = launch_diff_dq(p, wq, units * p.tiles, s);
+    if (err != hipSuccess)
+        return err;
+    const int64_t blocks = units * p.ktiles * p.rsplits;
+    p.dtype == 0 ? run_any<F32>(p, wk, blocks, s) : run_any<BF16>(p, wk, blocks, s);
+    err = hipGetLastError();
+    if (err != hipSuccess)
+        return err;
+    if (p.rsplits > 1) {
+        const dim3 grid(unsigned(units * p.nk));
+        if (p.dtype == 0)
+            diff_dkv_merge_kernel<F32><<<grid, kMerge, 0, s>>>(p);
+        else
+            diff_dkv_merge_kernel<BF16><<<grid, kMerge, 0, s>>>(p);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace nystra

@@ -1,0 +1,219 @@
+// Backward pass of differential attention, first half: dQ, row by row (the formulas stand
+// in diff_common.hpp).
+#include "diff_common.hpp"
+
+namespace nystra {
+namespace {
+
+using namespace diff;
+
+// Sum of the products of eight elements and eight fp32 values.
+template <class E>
+__device__ inline float dot8(const Frag<E> &a, const Chunk<F32> &b)
+{
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        s = fmaf(float(a.x[j]), __uint_as_float(b.w[j]), s);
+    return s;
+}
+
+// dQ, and per row D_1, D_2 and -dlam.  Rows as in the forward pass.  D_a comes from the
+// maps' outputs, D_2 = dO . O_2 and D_1 = dO . O_1 (fp32: dO . O + lam D_2), which the
+// forward pass keeps in fp32 (from outputs rounded to bf16, dQ was off by 0.0030 of its norm
+// at 4096 keys where rounding it alone costs 0.0017), or, where it kept none (few keys), from
+// a first walk over the keys.
+template <class E, int DK, int DV, int NW, bool DIRECT, bool KEPT>
+__global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>(!KEPT)))
+diff_dq_kernel(DiffProblem p)
+{
+    using T = typename E::T;
+    using Tiles = KeyTiles<E, DK, DV, 64 * NW, DIRECT>;
+    constexpr int KT = Tiles::KT;
+    __shared__ typename Tiles::Buffer buf[2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
+    const int64_t b = xcd_order(blockIdx.x, gridDim.x);
+    const int tile = int(b % p.tiles);
+    const int64_t unit = b / p.tiles;
+    const int w = int(unit / p.G), kvh = int(unit % p.G);
+    const int nrows = p.R * p.nq;
+    const int r0 = tile * 32 * NW, r = r0 + wave * 32 + c;
+    const bool live = r < nrows;
+    const Row row = row_of(p, kvh, live ? r : r0);
+    const int len = window_len(p, w);
+    const int limit = live ? key_limit(p, len, row.token) : 0;
+    const int r1 = min(r0 + 32 * NW, nrows) - 1;
+    const int kend = tile_limit(p, len, r0, r1);
+    const float lam = p.lambda[row.head];
+    const T *k0 = at<E>(p.k, w, 2 * kvh, 0), *v0 = at<E>(p.v, w, kvh, 0);
+
+    Tiles tiles;
+    if (kend > 0)
+        tiles.fetch(p, k0, v0, 0, kend, buf[0]);
+    Frag<E> q[2][DK / 16], go[DV / 16];
+    float L[2], D[2] = {0.f, 0.f};
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        const T *src = at<E>(p.q, w, 2 * row.head + a, row.token);
+#pragma unroll
+        for (int i = 0; i < DK / 16; ++i)
+            q[a][i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
+                                                       p.d - 16 * i - 8 * g, live, p.vec_q));
+        L[a] = limit > 0 ? p.lse[(int64_t(w) * 2 * p.H + 2 * row.head + a) * p.nq + row.token]
+                         : INFINITY;   // exp2(-inf) = 0 where no key is seen
+    }
+    const T *gosrc = at<E>(p.go, w, row.head, row.token);
+#pragma unroll
+    for (int i = 0; i < DV / 16; ++i)
+        go[i] = as_frag<E>(load_chunk<E, DIRECT>(gosrc + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
+                                                 live, p.vec_go));
+    if constexpr (KEPT) {
+        const float *o2 = map_row<E>(p, w, row);
+        const float *o1 = E::bytes == 2 ? o2 + p.dv : at<F32>(p.o, w, row.head, row.token);
+        const int vec2 = p.dv % 4 == 0 ? 16 : 4, vec1 = E::bytes == 2 ? vec2 : p.vec_o;
+#pragma unroll 2   // more would hold more of the rows at once than there are registers
+        for (int col = 8 * g; col < p.dv; col += 16) {
+            const int n = p.dv - col;
+            const Frag<E> x = as_frag<E>(load_chunk<E, DIRECT>(gosrc + col, n, live, p.vec_go));
+            D[0] += dot8(x, load_chunk<F32, false>(o1 + col, n, live, vec1));
+            D[1] += dot8(x, load_chunk<F32, false>(o2 + col, n, live, vec2));
+        }
+        if (E::bytes == 4)
+            D[0] = fmaf(lam, D[1], D[0]);
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+            D[a] += other_half(D[a]);
+    }
+    f16v acc[2][DK / 32] = {};
+    float glam = 0.f;
+    if (kend > 0)
+        tiles.commit(buf[0]);
+    int at_buf = 0;
+    for (int sweep = KEPT ? 1 : 0; sweep < 2; ++sweep) {
+        float sum[2] = {0.f, 0.f};
+        for (int key = 0; key < kend; key += KT, at_buf ^= 1) {
+            Tiles::ready();
+            const bool wrap = key + KT >= kend, more = !wrap || sweep == 0;
+            if (more)
+                tiles.fetch(p, k0, v0, wrap ? 0 : key + KT, kend, buf[at_buf ^ 1]);
+            const typename Tiles::Buffer &t = buf[at_buf];
+            if (__any(key < limit)) {
+                f16v s[2] = {}, x = {};
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+#pragma unroll
+                    for (int i = 0; i < DK / 16; ++i)
+                        s[a] = mma(row_frag<E, DK>(t.k[a], i), q[a][i], s[a]);
+                    part();
+                }
+#pragma unroll
+                for (int i = 0; i < DV / 16; ++i)
+                    x = mma(row_frag<E, DV>(t.v, i), go[i], x);
+                part();
+                if (!__all(key + KT <= limit)) {
+                    hide(s[0], limit, key, g);
+                    hide(s[1], limit, key, g);
+                }
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        s[a][i] = fast_exp2(fmaf(s[a][i], p.scale2, -L[a]));
+                if (sweep == 0) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        sum[0] = fmaf(s[0][i], x[i], sum[0]);
+                        sum[1] = fmaf(s[1][i], x[i], sum[1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        glam = fmaf(s[1][i], x[i], glam);
+                        s[0][i] *= x[i] - D[0];
+                        s[1][i] *= fmaf(-lam, x[i], lam * D[1]);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int a = 0; a < 2; ++a) {
+                            const Frag<E> ds = frag_of(s[a], h, E());
+#pragma unroll
+                            for (int i = 0; i < DK / 32; ++i)
+                                acc[a][i] = mma(col_frag<E, DK>(t.k[a], h, 32 * i), ds, acc[a][i]);
+                        }
+                }
+            }
+            if (more)
+                tiles.commit(buf[at_buf ^ 1]);
+        }
+        if (sweep == 0) {
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+                D[a] = sum[a] + other_half(sum[a]);
+        }
+    }
+    glam += other_half(glam);
+    // What the dK, dV kernel needs of a row, also for those up to the end of the last tile
+    // of 32.
+    if (g == 0 && r < p.rows32)
+        p.row_stats[unit * p.rows32 + r] = limit > 0 ? make_float4(L[0], L[1], D[0], D[1])
+                                                     : make_float4(L[0], L[1], 0.f, 0.f);
+    if (!live)
+        return;
+    if (g == 0)
+        p.rows_lam[unit * nrows + r] = glam;
+    // A softmax over one key is constant: its gradient is zero, not the rounding of D.
+    const float scale = limit == 1 ? 0.f : p.scale;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        T *dst = at_out<E>(p.gq, w, 2 * row.head + a, row.token);
+#pragma unroll
+        for (int i = 0; i < DK / 32; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                store4<E>(dst, 32 * i + 8 * t + 4 * g, p.d, p.vec_gq, scale * acc[a][i][4 * t],
+                          scale * acc[a][i][4 * t + 1], scale * acc[a][i][4 * t + 2],
+                          scale * acc[a][i][4 * t + 3]);
+    }
+}
+
+template <class E, int DK, int DV, int NW, bool DIRECT>
+void launch(const DiffProblem &p, int64_t blocks, hipStream_t s)
+{
+    const dim3 grid(unsigned(blocks), 1, 1);
+    if (p.maps)
+        diff_dq_kernel<E, DK, DV, NW, DIRECT, true><<<grid, 64 * NW, 0, s>>>(p);
+    else
+        diff_dq_kernel<E, DK, DV, NW, DIRECT, false><<<grid, 64 * NW, 0, s>>>(p);
+}
+
+template <class E, int DK, int DV, int NW>
+void run(const DiffProblem &p, int64_t blocks, hipStream_t s)
+{
+    if constexpr (E::bytes == 2) {
+        if (direct(p, p.q, p.d, 0) && direct(p, p.go, p.dv, 0) &&
+            direct(p, p.k, p.d, p.k.head + 32 * p.k.token) &&
+            direct(p, p.v, p.dv, 32 * p.v.token))
+            return launch<E, DK, DV, NW, true>(p, blocks, s);
+    }
+    launch<E, DK, DV, NW, false>(p, blocks, s);
+}
+
+template <class E>
+void run_any(const DiffProblem &p, int waves, int64_t blocks, hipStream_t s)
+{
+    if (waves == 2)
+        narrow(p) ? run<E, 32, 64, 2>(p, blocks, s) : run<E, 64, 128, 2>(p, blocks, s);
+    else
+        narrow(p) ? run<E, 32, 64, 4>(p, blocks, s) : run<E, 64, 128, 4>(p, blocks, s);
+}
+
+}  // namespace
+
+hipError_t launch_diff_dq(const DiffProblem &p, int waves, int64_t blocks, hipStream_t s)
+{
+    p.dtype == 0 ? run_any<F32>(p, waves, blocks, s) : run_any<BF16>(p, waves, blocks, s);
+    return hipGetLastError();
+}
+
+}  // namespace nystra

@@ -134,7 +134,7 @@ struct DiffView {
 // launcher's.
 struct DiffProblem {
     DiffView q, k, v, o, go, gq, gk, gv;   // Q and K hold two heads per query / key head
-    void *o2;              // [W][H][nq][dv], the second map's output, or null
+    float *maps;           // [W][H][nq][1 or 2][dv], the maps' outputs, or null
     float *lse;            // [W][2H][nq], log2 of the sums of exponentials, or null
     const float *lambda;   // [H]
     const int32_t *kv_len; // [W] or null
@@ -144,17 +144,23 @@ struct DiffProblem {
     int dtype;
     float scale, scale2;   // logit scale, and that times log2(e)
 
-    int vec_q, vec_k, vec_v, vec_go, vec_o, vec_o2;
-    bool vec_gq, vec_gk, vec_gv;
-    int tiles, ktiles, splits, chunk, dv4, partial_row;
-    float *partial, *rows_d1, *rows_d2, *rows_lam;
+    float *glam;           // [H], the gradient of lambda
+
+    uint32_t nq_mul;       // division by nq
+    int nq_shift;
+    int vec_q, vec_k, vec_v, vec_go, vec_o;
+    bool store_o, vec_gq, vec_gk, vec_gv;
+    int tiles, ktiles, splits, chunk, rsplits, rchunk, d4, dv4, partial_row;
+    int64_t rows32;        // rows of a unit, up to a multiple of 32
+    float *partial, *rows_lam;
+    float4 *row_stats;     // [units][rows32]: L_1, L_2, D_1, D_2
 };
 // Whether the grids of a call stay under the limits of a launch.
 bool diff_grid_fits(const DiffProblem &p);
 size_t diff_forward_workspace(const DiffProblem &p);
 size_t diff_backward_workspace(const DiffProblem &p);
 hipError_t launch_diff_forward(DiffProblem p, void *workspace, hipStream_t stream);
-hipError_t launch_diff_backward(DiffProblem p, void *workspace, float *glam, hipStream_t stream);
+hipError_t launch_diff_backward(DiffProblem p, void *workspace, hipStream_t stream);
 
 // Head widths with a tiled instantiation: the multiples of 4 from 8 to 32
 // (Dehazeformer's 12 and 16, Uformer's 32) and SwinIR's 30.

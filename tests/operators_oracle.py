@@ -126,16 +126,14 @@ def diff_attention(q, k, v, lam, causal=0, kv_len=None, scale=None, do=None, sho
     aX = g.abs() @ v64.abs().transpose(-1, -2)
     eX = EPS32 * (dv + 8) * aX
     D = [(p * X).sum(-1, keepdim=True) for p in P]
-    O2, P2V = P[1] @ v64, P[1] @ v64.abs()
     if nk > short:
-        # from the stored outputs: dO . O_2 and dO . (O + lam O_2), each stored value off
-        # by its rounding and by its products' operands
-        eo = half * O.abs() + eO * (1 + half)
-        eo2 = half * O2.abs() + (low + eP + eAcc) * P2V * (1 + half)
+        # dO . O_a from the fp32 outputs: off by their products' operands and their sums
         dot = EPS32 * (dv + 8)
-        eD2 = (g.abs() * (eo2 + dot * O2.abs())).sum(-1, keepdim=True)
-        eD1 = (g.abs() * (eo + dot * O.abs())).sum(-1, keepdim=True) + l.abs() * eD2
-        eD = [eD1, eD2]
+        eD = [(g.abs() * ((low + eP + eAcc) * (p @ v64.abs()) + dot * (p @ v64).abs()))
+              .sum(-1, keepdim=True) for p in P]
+        if dt == torch.float32:      # D_1 from O and D_2
+            eD[0] = ((g.abs() * (eO + (dot + half) * O.abs())).sum(-1, keepdim=True) +
+                     l.abs() * eD[1])
     else:
         eD = [(p * (eX + (eP + EPS32 * (nk + 8)) * X.abs())).sum(-1, keepdim=True) for p in P]
     w = [1.0, -l]
