@@ -18,7 +18,8 @@ diff_forward_kernel(DiffProblem p)
     using T = typename E::T;
     using Tiles = KeyTiles<E, DK, DV, 64 * NW, DIRECT>;
     constexpr int KT = Tiles::KT;
-    __shared__ typename Tiles::Buffer buf[2];
+    __shared__ alignas(256) char lds[2 * Tiles::kBuffer];
+    const uint32_t buf = lds_offset(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
     int64_t b = xcd_order(blockIdx.x, gridDim.x);
     const int split = int(b % p.splits);
@@ -39,7 +40,7 @@ diff_forward_kernel(DiffProblem p)
 
     Tiles tiles;
     if (kbegin < kend)
-        tiles.fetch(p, k0, v0, kbegin, kend, buf[0]);
+        tiles.fetch(p, k0, v0, kbegin, kend, buf);
     Frag<E> q[2][DK / 16];
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
@@ -47,28 +48,28 @@ diff_forward_kernel(DiffProblem p)
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
             q[a][i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
-                                                       p.d - 16 * i - 8 * g, live, p.vec_q));
+                                                       p.d - 16 * i - 8 * g, live, p.d));
     }
     f16v acc[2][DV / 32] = {};
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     if (kbegin < kend)
-        tiles.commit(buf[0]);
+        tiles.commit(buf);
 
-    for (int key = kbegin, at_buf = 0; key < kend; key += KT, at_buf ^= 1) {
+    uint32_t t = buf, other = buf + Tiles::kBuffer;   // this tile's buffer and the next one's
+    for (int key = kbegin; key < kend; key += KT) {
         Tiles::ready();
         const bool more = key + KT < kend;
         if (more)
-            tiles.fetch(p, k0, v0, key + KT, kend, buf[at_buf ^ 1]);
-        const typename Tiles::Buffer &t = buf[at_buf];
+            tiles.fetch(p, k0, v0, key + KT, kend, other);
         if (__any(key < limit)) {
+            const uint32_t krow = first_row<E, DK>(t), vcol = first_col<E, DV>(t + Tiles::kV);
             f16v s[2] = {};
 #pragma unroll
-            for (int a = 0; a < 2; ++a) {
+            for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
-                for (int i = 0; i < DK / 16; ++i)
-                    s[a] = mma(row_frag<E, DK>(t.k[a], i), q[a][i], s[a]);
-                part();
-            }
+                for (int a = 0; a < 2; ++a)
+                    s[a] = mma(row_frag<E>(krow + a * KT * Tiles::LK::pitch, i), q[a][i], s[a]);
+            part();
             if (!__all(key + KT <= limit)) {
                 hide(s[0], limit, key, g);
                 hide(s[1], limit, key, g);
@@ -85,18 +86,19 @@ diff_forward_kernel(DiffProblem p)
                 const Frag<E> p1 = frag_of(s[0], h, E()), p2 = frag_of(s[1], h, E());
 #pragma unroll
                 for (int i = 0; i < DV / 32; ++i) {
-                    const Frag<E> v = col_frag<E, DV>(t.v, h, 32 * i);
+                    const Frag<E> v = col_frag<E, DV>(vcol, h, i);
                     acc[0][i] = mma(v, p1, acc[0][i]);
                     acc[1][i] = mma(v, p2, acc[1][i]);
                 }
             }
         }
         if (more)
-            tiles.commit(buf[at_buf ^ 1]);
+            tiles.commit(other);
+        exchange(t, other);
     }
 #pragma unroll
     for (int a = 0; a < 2; ++a)
-        l[a] += other_half(l[a]);
+        l[a] = half_sum(l[a]);
     if (!live)
         return;
     if (p.splits > 1) {

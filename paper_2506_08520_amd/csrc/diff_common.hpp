@@ -33,6 +33,8 @@ namespace diff {
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 template <class E>
 struct Frag;
@@ -66,44 +68,64 @@ struct alignas(16) Chunk {
     uint32_t w[2 * E::bytes];
 };
 
+// 16 bytes from an address that is aligned to the element only.
+template <class E>
+struct __attribute__((packed, aligned(E::bytes))) Loose {
+    uint32_t w[4];
+};
+
 // Eight elements of a row from p, of which the row has n (n may be <= 0 or above 8); the
-// others, and all of them if the row is not `live`, are zero.  Every lane loads, from the
-// row's last elements where its own are not there, so that there are no branches.  WIDE:
-// rows are whole aligned 16-byte chunks; otherwise loads are of `vec` bytes (4 or the
-// element's for bf16, 16 or 4 for fp32), which divide the row's start and width.
+// others, and all of them if the row is not `live`, are zero.  Every lane loads 16 bytes at a
+// time, from the row's last ones where its own would reach past the row, and shifts those
+// down, so that there are no branches and nothing is read outside the row.  WIDE: n is a
+// multiple of eight and the address of 16 bytes.  `width`: the row's elements, of which
+// fewer than 16 bytes are taken one by one.
 template <class E, bool WIDE>
-__device__ inline Chunk<E> load_chunk(const typename E::T *p, int n, bool live, int vec)
+__device__ inline Chunk<E> load_chunk(const typename E::T *p, int n, bool live, int width)
 {
+    constexpr int per = 16 / E::bytes;
     Chunk<E> c;
-    if (E::bytes == 2 && WIDE) {
-        const uint4 u = *reinterpret_cast<const uint4 *>(p + min(0, n - 8));
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            c.w[j] = live && n > 0 ? w[j] : 0u;
-    } else if (E::bytes == 4 && vec == 16) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(p + min(4 * h, n - 4));
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    for (int h = 0; h < 8 / per; ++h) {
+        const int left = n - h * per;   // elements of the row from here on
+        uint32_t w[4];
+        if (WIDE) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(p + min(0, left - per));
+            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+        } else if (width >= per) {
+            const Loose<E> u =
+                *reinterpret_cast<const Loose<E> *>(p + h * per + min(0, left - per));
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                c.w[4 * h + j] = live && 4 * h < n ? w[j] : 0u;
-        }
-    } else if (E::bytes == 4 || vec == 4) {
-        constexpr int per = 4 / E::bytes;
+                w[j] = u.w[j];
+            if (width % per != 0) {
+                const int skip = max(0, per - left) * E::bytes;   // bytes, below 16 where live
+                if (skip & 8)
+                    w[0] = w[2], w[1] = w[3], w[2] = w[3] = 0u;
+                if (skip & 4)
+                    w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = 0u;
+                if (E::bytes == 2 && skip & 2)
+                    w[0] = w[0] >> 16 | w[1] << 16, w[1] = w[1] >> 16 | w[2] << 16,
+                    w[2] = w[2] >> 16 | w[3] << 16, w[3] >>= 16;
+            }
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8 / per; ++j) {
-            const uint32_t u = *reinterpret_cast<const uint32_t *>(p + min(j * per, n - per));
-            c.w[j] = live && j * per < n ? u : 0u;
+            for (int j = 0; j < per; ++j) {
+                uint32_t u = 0;
+                if (E::bytes == 4)
+                    u = *reinterpret_cast<const uint32_t *>(p + h * per + min(j, left - 1));
+                else
+                    u = *reinterpret_cast<const uint16_t *>(p + h * per + min(j, left - 1));
+                u = j < left ? u : 0u;
+                if (E::bytes == 4)
+                    w[j] = u;
+                else
+                    w[j / 2] = j & 1 ? w[j / 2] | u << 16 : u;
+            }
         }
-    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            uint32_t u = *reinterpret_cast<const uint16_t *>(p + min(j, n - 1));
-            u = live && j < n ? u : 0u;
-            c.w[j * E::bytes / 4] = j & 1 ? c.w[j * E::bytes / 4] | u << 16 : u;
-        }
+        for (int j = 0; j < 4; ++j)
+            c.w[4 * h + j] = live && left > 0 ? w[j] : 0u;
     }
     return c;
 }
@@ -133,14 +155,58 @@ __device__ inline Frag<F32> frag_of(const f16v &s, int c, F32)
     return f;
 }
 
+// LDS is addressed by byte offsets.
+__device__ inline uint32_t lds_offset(void *p)
+{
+    return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void *)p));
+}
+
+template <class T>
+__device__ inline __attribute__((address_space(3))) T *lds_at(uint32_t at)
+{
+    return (__attribute__((address_space(3))) T *)(uintptr_t(at));
+}
+
+template <class E>
+__device__ inline Chunk<E> lds_chunk(uint32_t at)
+{
+    Chunk<E> c;
+#pragma unroll
+    for (int h = 0; h < E::bytes / 2; ++h) {
+        const u4 x = *lds_at<u4>(at + 16 * h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            c.w[4 * h + j] = x[j];
+    }
+    return c;
+}
+
+template <class E>
+__device__ inline void set_lds_chunk(uint32_t at, const Chunk<E> &c)
+{
+#pragma unroll
+    for (int h = 0; h < E::bytes / 2; ++h)
+        *lds_at<u4>(at + 16 * h) =
+            (u4){c.w[4 * h], c.w[4 * h + 1], c.w[4 * h + 2], c.w[4 * h + 3]};
+}
+
+__device__ inline void exchange(uint32_t &a, uint32_t &b)
+{
+    const uint32_t x = a;
+    a = b;
+    b = x;
+}
+
 // A tile of rows of COLS elements in LDS, in chunks of eight elements.  Row fragments read
 // the same chunk of eight rows at a time, the transposing reads below two neighbouring
 // chunks of four rows; over the 64 banks of 4 bytes neither may meet a bank twice.  bf16
 // rows lie without gaps (so that loads can go to LDS directly) with their chunks exchanged
 // by a number from the row; fp32 rows, which have no transposing reads, are 16 bytes apart.
+// A bf16 tile starts at a multiple of 256 bytes, so that the fragments of a tile follow
+// from the first one's address by an exclusive or (one instruction and no register each).
 template <class E, int COLS>
 struct Tile {
-    static constexpr int pitch = E::bytes == 2 ? COLS : COLS + 4;
+    static constexpr int pitch = E::bytes == 2 ? 2 * COLS : 4 * COLS + 16;   // bytes
     static constexpr int kRow = COLS / 8;
 
     __device__ static inline int swap(int row)
@@ -150,48 +216,66 @@ struct Tile {
         else
             return COLS == 32 ? (row >> 2) & 3 : COLS == 64 ? row & 7 : (row & 7) << 1;
     }
-    __device__ static inline int at(int row, int chunk)
+    __device__ static inline uint32_t at(int row, int chunk)
     {
-        return row * pitch + 8 * (chunk ^ swap(row));
+        return row * pitch + 8 * E::bytes * (chunk ^ swap(row));
     }
 };
 
-// Row lane % 32 of a tile, contraction indices (columns) 16 c + 8 g + j.
+// Row fragments: row lane % 32 of the tile at `tile`, contraction indices (columns)
+// 16 c + 8 g + j.  first_row() gives the address for c = 0.
 template <class E, int COLS>
-__device__ inline Frag<E> row_frag(const typename E::T *tile, int c)
+__device__ inline uint32_t first_row(uint32_t tile)
 {
     const int lane = threadIdx.x & 63;
-    return as_frag<E>(*reinterpret_cast<const Chunk<E> *>(
-        tile + Tile<E, COLS>::at(lane & 31, 2 * c + (lane >> 5))));
+    return tile + Tile<E, COLS>::at(lane & 31, lane >> 5);
 }
 
-// Column col0 + lane % 32 of a tile, contraction indices (rows) in the order of a
-// product's result: 16 c + 8 (j / 4) + 4 g + j % 4.  In bf16 the transposing LDS
-// read takes four rows of 16 columns from 16 lanes (lane p: row p / 4, columns
-// 4 (p % 4) ..) and gives each lane its column of them.
-template <class E, int COLS>
-__device__ inline Frag<E> col_frag(const typename E::T *tile, int c, int col0)
+template <class E>
+__device__ inline Frag<E> row_frag(uint32_t first, int c)
 {
-    using L = Tile<E, COLS>;
+    if constexpr (E::bytes == 2) {
+        return as_frag<E>(lds_chunk<E>(first ^ (32 * c)));
+    } else {
+        return as_frag<E>(lds_chunk<E>(first + 64 * c));
+    }
+}
+
+// Column fragments: column 32 i + lane % 32, contraction indices (rows) in the order of a
+// product's result, 16 c + 8 (j / 4) + 4 g + j % 4.  In bf16 the transposing LDS read
+// takes four rows of 16 columns from 16 lanes (lane p: row p / 4, columns 4 (p % 4) ..) and
+// gives each lane its column of them.
+template <class E, int COLS>
+__device__ inline uint32_t first_col(uint32_t tile)
+{
     const int lane = threadIdx.x & 63, g = lane >> 5;
     if constexpr (E::bytes == 2) {
-        typedef __attribute__((address_space(3))) s4 ls4;
-        const int row = 16 * c + 4 * g + ((lane & 15) >> 2);
-        const int col = col0 + (lane & 16) + 4 * (lane & 3);
+        const int col = (lane & 16) + 4 * (lane & 3);
+        return tile + Tile<E, COLS>::at(4 * g + ((lane & 15) >> 2), col >> 3) + 2 * (col & 7);
+    } else {
+        return tile + 4 * g * Tile<E, COLS>::pitch + 4 * (lane & 31);
+    }
+}
+
+template <class E, int COLS>
+__device__ inline Frag<E> col_frag(uint32_t first, int c, int i)
+{
+    constexpr int pitch = Tile<E, COLS>::pitch;
+    if constexpr (E::bytes == 2) {
+        const uint32_t lo = (first ^ (64 * i)) + 16 * c * pitch;
+        // Eight rows on, rows of four chunks have theirs exchanged by another number.
+        const uint32_t hi = (COLS == 32 ? first ^ 32 : first ^ (64 * i)) + (16 * c + 8) * pitch;
         struct {
             s4 lo, hi;
         } v;
-        v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (ls4 *)(tile + L::at(row, col >> 3) + (col & 7)));
-        v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (ls4 *)(tile + L::at(row + 8, col >> 3) + (col & 7)));
+        v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s4>(lo));
+        v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s4>(hi));
         return __builtin_bit_cast(Frag<BF16>, v);
     } else {
         Frag<F32> f;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            f.x[j] = tile[(16 * c + 8 * (j >> 2) + 4 * g + (j & 3)) * L::pitch + col0 +
-                          (lane & 31)];
+            f.x[j] = *lds_at<float>(first + (16 * c + 8 * (j >> 2) + (j & 3)) * pitch + 128 * i);
         return f;
     }
 }
@@ -209,36 +293,34 @@ struct Stage {
     // at(row) points to the first element of a row, live(row) says whether it is there.
     // Row 0 is always there.
     template <class At, class Live>
-    __device__ inline void load(At at, Live live, int cols, int vec)
+    __device__ inline void load(At at, Live live, int cols)
     {
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             const int id = threadIdx.x + i * NT;
             const int row = id / L::kRow % ROWS, col = id % L::kRow * 8;
             const bool in = live(row);
-            x[i] = load_chunk<E, false>(at(in ? row : 0) + col, cols - col, in, vec);
+            x[i] = load_chunk<E, false>(at(in ? row : 0) + col, cols - col, in, cols);
         }
     }
 
-    __device__ inline void store(typename E::T *lds) const
+    __device__ inline void store(uint32_t lds) const
     {
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             const int id = threadIdx.x + i * NT;
             if (kAll % NT == 0 || id < kAll)
-                *reinterpret_cast<Chunk<E> *>(lds + L::at(id / L::kRow, id % L::kRow)) = x[i];
+                set_lds_chunk<E>(lds + L::at(id / L::kRow, id % L::kRow), x[i]);
         }
     }
 };
 
 // 16 bytes from `base` plus each lane's offset to LDS, lane after lane from `lds` on, past
 // the registers.  Nothing waits for it but arrived().  base and lds are the wave's.
-__device__ inline void load_to_lds(const void *base, uint32_t offset, void *lds)
+__device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t lds)
 {
-    const uint32_t to = __builtin_amdgcn_readfirstlane(
-        uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void *)lds)));
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 :: "s"(to), "v"(offset), "s"(base) : "memory");
+                 :: "s"(lds), "v"(offset), "s"(base) : "memory");
 }
 
 __device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
@@ -248,7 +330,7 @@ __device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory
 // not there must be given as another's (their products are masked), and columns from `cols`
 // on hold the last chunk again (the other operand is zero there).
 template <int COLS, int ROWS, int NT, class At>
-__device__ inline void direct_tile(uint16_t *lds, const void *base, At at, int cols)
+__device__ inline void direct_tile(uint32_t lds, const void *base, At at, int cols)
 {
     using L = Tile<BF16, COLS>;
     static_assert(ROWS * L::kRow % NT == 0, "whole waves");
@@ -257,13 +339,34 @@ __device__ inline void direct_tile(uint16_t *lds, const void *base, At at, int c
         const int id = threadIdx.x + i * NT;
         const int row = id / L::kRow, chunk = id % L::kRow ^ L::swap(row);
         const int col = min(8 * chunk, cols - 8);
-        load_to_lds(base, 2 * uint32_t(at(row) + col), lds + (i * NT + (threadIdx.x & ~63u)) * 8);
+        load_to_lds(base, 2 * uint32_t(at(row) + col),
+                    __builtin_amdgcn_readfirstlane(lds + 16 * (i * NT + (threadIdx.x & ~63u))));
     }
 }
 
-__device__ inline float other_half(float x)
+// The values of lanes c and c + 32, the same in both.
+struct Halves {
+    float lo, hi;
+};
+
+__device__ inline Halves halves(float x)
 {
-    return __shfl_xor(x, 32, 64);
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return Halves{__builtin_bit_cast(float, unsigned(r[0])),
+                  __builtin_bit_cast(float, unsigned(r[1]))};
+}
+
+__device__ inline float half_sum(float x)
+{
+    const Halves h = halves(x);
+    return h.lo + h.hi;
+}
+
+__device__ inline float half_max(float x)
+{
+    const Halves h = halves(x);
+    return fmaxf(h.lo, h.hi);
 }
 
 // r / n_q for 0 <= r < 2^30: with k = 31 + floor(log2 n_q) and M = ceil(2^k / n_q), M n_q
@@ -335,7 +438,6 @@ __device__ inline void store4(typename E::T *row, int col, int n, bool vec, floa
             if constexpr (E::bytes == 4) {
                 *reinterpret_cast<float4 *>(row + col) = make_float4(a, b, c, d);
             } else {
-                typedef float f4 __attribute__((ext_vector_type(4)));
                 typedef __bf16 b4 __attribute__((ext_vector_type(4)));
                 *reinterpret_cast<b4 *>(row + col) = __builtin_convertvector((f4{a, b, c, d}), b4);
             }
@@ -385,7 +487,7 @@ __device__ inline void softmax_step(f16v &s, float scale2, float &m, float &l, G
 #pragma unroll
     for (int r = 1; r < 16; ++r)
         t = fmaxf(t, s[r]);
-    t = fmaxf(t, other_half(t)) * scale2;
+    t = half_max(t) * scale2;
     if (__any(t > m + 8.f)) {
         const float mn = fmaxf(m, t);
         // A row that has seen no key yet has nothing to rescale.
@@ -421,15 +523,13 @@ struct KeyTiles {
     using T = typename E::T;
     using LK = Tile<E, DK>;
     using LV = Tile<E, DV>;
-    struct Buffer {
-        alignas(16) T k[2][KT * LK::pitch];
-        alignas(16) T v[KT * LV::pitch];
-    };
+    // One buffer in LDS: the keys of both maps, then the values.
+    static constexpr uint32_t kV = 2 * KT * LK::pitch, kBuffer = kV + KT * LV::pitch;
     Stage<E, DK, 2 * KT, NT> k;   // both maps, one under the other
     Stage<E, DV, KT, NT> v;
 
     __device__ inline void fetch(const DiffProblem &p, const T *k0, const T *v0, int key, int end,
-                                 Buffer &to)
+                                 uint32_t to)
     {
         const int last = end - key - 1;
         k0 += key * p.k.token;
@@ -437,22 +537,22 @@ struct KeyTiles {
         if constexpr (DIRECT) {
             const int kh = int(p.k.head), kt = int(p.k.token), vt = int(p.v.token);
             direct_tile<DK, 2 * KT, NT>(
-                to.k[0], k0, [&](int row) { return (row / KT) * kh + min(row % KT, last) * kt; },
+                to, k0, [&](int row) { return (row / KT) * kh + min(row % KT, last) * kt; },
                 p.d);
-            direct_tile<DV, KT, NT>(to.v, v0, [&](int row) { return min(row, last) * vt; }, p.dv);
+            direct_tile<DV, KT, NT>(to + kV, v0, [&](int row) { return min(row, last) * vt; }, p.dv);
         } else {
             k.load([&](int row) { return k0 + (row / KT) * p.k.head + (row % KT) * p.k.token; },
-                   [&](int row) { return row % KT <= last; }, p.d, p.vec_k);
+                   [&](int row) { return row % KT <= last; }, p.d);
             v.load([&](int row) { return v0 + row * p.v.token; },
-                   [&](int row) { return row <= last; }, p.dv, p.vec_v);
+                   [&](int row) { return row <= last; }, p.dv);
         }
     }
 
-    __device__ inline void commit(Buffer &to) const
+    __device__ inline void commit(uint32_t to) const
     {
         if constexpr (!DIRECT) {
-            k.store(to.k[0]);
-            v.store(to.v);
+            k.store(to);
+            v.store(to + kV);
         }
     }
 
@@ -486,14 +586,6 @@ inline bool aligned(const DiffView &v, int width, int bytes, int to)
            (v.window | v.head | v.token | width) * bytes % to == 0;
 }
 
-// Bytes of one load where rows are not whole 16-byte chunks of bf16 (see load_chunk).
-inline int view_vec(const DiffView &v, int width, int bytes)
-{
-    if (bytes == 4)
-        return aligned(v, width, 4, 16) ? 16 : 4;
-    return aligned(v, width, 2, 4) ? 4 : 2;
-}
-
 // Whether tiles can be loaded to LDS directly: bf16 rows of whole 16-byte chunks, and
 // `span` elements, those of a tile or of a unit, within 32-bit offsets.
 inline bool direct(const DiffProblem &p, const DiffView &v, int width, int64_t span)
@@ -519,10 +611,6 @@ inline bool narrow(const DiffProblem &p) { return p.d <= 32 && p.dv <= 64; }
 
 inline void set_common(DiffProblem *p)
 {
-    const int e = p->dtype == 0 ? 4 : 2;
-    p->vec_q = view_vec(p->q, p->d, e);
-    p->vec_k = view_vec(p->k, p->d, e);
-    p->vec_v = view_vec(p->v, p->dv, e);
     p->nq_shift = 31 + (31 - __builtin_clz(unsigned(p->nq)));
     p->nq_mul = uint32_t(((uint64_t(1) << p->nq_shift) + p->nq - 1) / p->nq);
 }

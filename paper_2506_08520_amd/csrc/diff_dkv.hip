@@ -22,6 +22,7 @@ __device__ inline void sum_dlam(const DiffProblem &p, int h, float *out)
     __shared__ float lds[NT / 64];
     float s = 0.f;
     const int n = p.W * p.nq;   // below 2^24
+#pragma unroll 8   // loads in flight: the rows are far more than the threads
     for (int i = threadIdx.x; i < n; i += NT) {
         const int w = div_nq(p, i);
         s += p.rows_lam[(int64_t(w) * p.H + h) * p.nq + (i - w * p.nq)];
@@ -41,7 +42,7 @@ __device__ inline void sum_dlam(const DiffProblem &p, int h, float *out)
 // dK and dV: a wave owns 32 keys and walks over the unit's rows, so that the heads
 // that share the keys are summed in registers.  Keys at or behind the window's
 // length get zeros.  With few workgroups the rows are split over p.rsplits of them, whose
-// sums go to the workspace.  The last H workgroups add up dlam meanwhile.
+// sums go to the workspace.  The first H workgroups add up dlam meanwhile.
 template <class E, int DK, int DV, int NW, bool DIRECT>
 __global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>()))
 diff_dkv_kernel(DiffProblem p)
@@ -52,22 +53,19 @@ diff_dkv_kernel(DiffProblem p)
     using LG = Tile<E, DV>;
     // The values' fragments stay in registers unless that halves the occupancy.
     constexpr bool kLdsV = E::bytes == 2 && DV == 128;
-    struct Buffer {
-        alignas(16) T q[2][QT * LQ::pitch];
-        alignas(16) T go[QT * LG::pitch];
-        float4 stat[QT];                  // L_1, L_2, D_1, D_2
-        alignas(16) float lam[QT];
-        alignas(16) int lim[QT];
-    };
-    __shared__ Buffer buf[2];
-    __shared__ alignas(16) T vs[kLdsV ? NW * 32 * LG::pitch : 8];
-    const int64_t blocks = int64_t(gridDim.x) - p.H;
-    if (int64_t(blockIdx.x) >= blocks) {
-        sum_dlam<NT>(p, int(blockIdx.x - blocks), p.glam);
+    // A buffer in LDS: the queries of both maps, dO, and per row L_1, L_2, D_1, D_2, lam
+    // and the keys that it sees.
+    constexpr uint32_t kMap = QT * LQ::pitch, kGo = 2 * kMap, kStat = kGo + QT * LG::pitch;
+    constexpr uint32_t kLam = kStat + 16 * QT, kLim = kLam + 4 * QT;
+    constexpr uint32_t kBuffer = (kLim + 4 * QT + 255) / 256 * 256;
+    __shared__ alignas(256) char lds[2 * kBuffer + (kLdsV ? NW * 32 * LG::pitch : 0)];
+    const uint32_t buf = lds_offset(lds), vs = buf + 2 * kBuffer;
+    if (int(blockIdx.x) < p.H) {
+        sum_dlam<NT>(p, blockIdx.x, p.glam);
         return;
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
-    int64_t b = xcd_order(blockIdx.x, blocks);
+    int64_t b = xcd_order(blockIdx.x - p.H, gridDim.x - p.H);
     const int split = int(b % p.rsplits);
     b /= p.rsplits;
     const int tile = int(b % p.ktiles);
@@ -85,7 +83,7 @@ diff_dkv_kernel(DiffProblem p)
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
             k[a][i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
-                                                       p.d - 16 * i - 8 * g, live, p.vec_k));
+                                                       p.d - 16 * i - 8 * g, live, p.d));
     }
     if constexpr (kLdsV) {
         const T *v0 = at<E>(p.v, w, kvh, 0);
@@ -94,21 +92,22 @@ diff_dkv_kernel(DiffProblem p)
         for (int i = 0; i < kChunks; ++i) {
             const int id = threadIdx.x + i * NT, row = id / LG::kRow, ch = id % LG::kRow;
             const bool in = kb + row < len;
-            *reinterpret_cast<Chunk<E> *>(vs + LG::at(row, ch)) = load_chunk<E, DIRECT>(
-                v0 + (in ? kb + row : 0) * p.v.token + 8 * ch, p.dv - 8 * ch, in, p.vec_v);
+            set_lds_chunk<E>(vs + LG::at(row, ch),
+                             load_chunk<E, DIRECT>(v0 + (in ? kb + row : 0) * p.v.token + 8 * ch,
+                                                   p.dv - 8 * ch, in, p.dv));
         }
     } else {
         const T *src = at<E>(p.v, w, kvh, live ? key : 0);
 #pragma unroll
         for (int i = 0; i < DV / 16; ++i)
             v[i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
-                                                    live, p.vec_v));
+                                                    live, p.dv));
     }
     f16v gk[2][DK / 32] = {}, gv[DV / 32] = {};
 
     Stage<E, DK, 2 * QT, NT> sq;
     Stage<E, DV, QT, NT> sgo;
-    float4 sstat;
+    f4 sstat;
     float slam;
     // Tiles of rows from `from` on, past those that see no key of this workgroup.
     const int rend = min(nrows, (split + 1) * p.rchunk);
@@ -129,72 +128,78 @@ diff_dkv_kernel(DiffProblem p)
         const Row row = row_of(p, 0, min(r, nrows - 1));
         return row.head * Off(p.go.head) + row.token * Off(p.go.token);
     };
-    auto fetch = [&](int r0, Buffer &t) {
+    auto fetch = [&](int r0, uint32_t t) {
         if constexpr (DIRECT) {
             direct_tile<DK, 2 * QT, NT>(
-                t.q[0], q0, [&](int i) { return q_row(r0 + i % QT, i / QT); }, p.d);
-            direct_tile<DV, QT, NT>(t.go, go0, [&](int i) { return go_row(r0 + i); }, p.dv);
+                t, q0, [&](int i) { return q_row(r0 + i % QT, i / QT); }, p.d);
+            direct_tile<DV, QT, NT>(t + kGo, go0, [&](int i) { return go_row(r0 + i); }, p.dv);
         } else {
             sq.load([&](int i) { return q0 + q_row(r0 + i % QT, i / QT); },
-                    [&](int i) { return r0 + i % QT < nrows; }, p.d, p.vec_q);
+                    [&](int i) { return r0 + i % QT < nrows; }, p.d);
             sgo.load([&](int i) { return go0 + go_row(r0 + i); },
-                     [&](int i) { return r0 + i < nrows; }, p.dv, p.vec_go);
+                     [&](int i) { return r0 + i < nrows; }, p.dv);
         }
         if (threadIdx.x < QT) {
-            sstat = p.row_stats[unit * p.rows32 + r0 + threadIdx.x];
+            const float4 *stats = p.row_stats + unit * p.rows32 + r0;
+            if constexpr (DIRECT)
+                load_to_lds(stats, 16 * threadIdx.x, t + kStat);
+            else
+                sstat = *reinterpret_cast<const f4 *>(stats + threadIdx.x);
             slam = p.lambda[row_of(p, kvh, min(r0 + int(threadIdx.x), nrows - 1)).head];
         }
     };
-    auto commit = [&](int r0, Buffer &t) {
+    auto commit = [&](int r0, uint32_t t) {
         if constexpr (!DIRECT) {
-            sq.store(t.q[0]);
-            sgo.store(t.go);
+            sq.store(t);
+            sgo.store(t + kGo);
         }
         if (threadIdx.x < QT) {
             const int r = r0 + threadIdx.x;
-            t.stat[threadIdx.x] = sstat;
-            t.lam[threadIdx.x] = slam;
-            t.lim[threadIdx.x] =
+            if constexpr (!DIRECT)
+                *lds_at<f4>(t + kStat + 16 * threadIdx.x) = sstat;
+            *lds_at<float>(t + kLam + 4 * threadIdx.x) = slam;
+            *lds_at<int>(t + kLim + 4 * threadIdx.x) =
                 r < nrows ? key_limit(p, len, row_of(p, kvh, r).token) : 0;
         }
     };
     int r0 = kb < len ? next(split * p.rchunk) : rend;
     if (r0 < rend) {
-        fetch(r0, buf[0]);
-        commit(r0, buf[0]);
+        fetch(r0, buf);
+        commit(r0, buf);
     }
-    for (int at_buf = 0; r0 < rend; at_buf ^= 1) {
+    uint32_t t = buf, other = buf + kBuffer;   // this tile's buffer and the next one's
+    while (r0 < rend) {
         if constexpr (DIRECT)
             arrived();
         __syncthreads();
         const int r1 = next(r0 + QT);
         if (r1 < rend)
-            fetch(r1, buf[at_buf ^ 1]);
-        const Buffer &t = buf[at_buf];
-        const int rowlim = t.lim[c];
+            fetch(r1, other);
+        const int rowlim = *lds_at<int>(t + kLim + 4 * c);
         if (__any(kw < rowlim)) {
             const bool masked = !__all(kw + 32 <= rowlim);
+            const uint32_t qrow = first_row<E, DK>(t), qcol = first_col<E, DK>(t);
+            const uint32_t grow = first_row<E, DV>(t + kGo), gcol = first_col<E, DV>(t + kGo);
             f16v s[2] = {}, x = {};
 #pragma unroll
-            for (int a = 0; a < 2; ++a) {
+            for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
-                for (int i = 0; i < DK / 16; ++i)
-                    s[a] = mma(row_frag<E, DK>(t.q[a], i), k[a][i], s[a]);
-                part();
-            }
+                for (int a = 0; a < 2; ++a)
+                    s[a] = mma(row_frag<E>(qrow + a * kMap, i), k[a][i], s[a]);
+            part();
 #pragma unroll
             for (int i = 0; i < DV / 16; ++i) {
                 if constexpr (kLdsV)
-                    x = mma(row_frag<E, DV>(t.go, i),
-                            row_frag<E, DV>(vs + wave * 32 * LG::pitch, i), x);
+                    x = mma(row_frag<E>(grow, i),
+                            row_frag<E>(first_row<E, DV>(vs + wave * 32 * LG::pitch), i), x);
                 else
-                    x = mma(row_frag<E, DV>(t.go, i), v[i], x);
+                    x = mma(row_frag<E>(grow, i), v[i], x);
             }
             part();
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const bool see = key < t.lim[reg_row(i, g)];
+                    const bool see = key < *lds_at<int>(t + kLim + 4 * reg_row(i, g));
                     s[0][i] = see ? s[0][i] : -INFINITY;
                     s[1][i] = see ? s[1][i] : -INFINITY;
                 }
@@ -202,12 +207,11 @@ diff_dkv_kernel(DiffProblem p)
             f16v pd;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float4 lm = *reinterpret_cast<const float4 *>(t.lam + 8 * j + 4 * g);
-                const float lam[4] = {lm.x, lm.y, lm.z, lm.w};
+                const f4 lam = *lds_at<f4>(t + kLam + 4 * (8 * j + 4 * g));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = 4 * j + e;
-                    const float4 st = t.stat[reg_row(i, g)];
+                    const f4 st = *lds_at<f4>(t + kStat + 16 * reg_row(i, g));
                     const float p1 = fast_exp2(fmaf(s[0][i], p.scale2, -st.x));
                     const float p2 = lam[e] * fast_exp2(fmaf(s[1][i], p.scale2, -st.y));
                     pd[i] = p1 - p2;
@@ -218,7 +222,7 @@ diff_dkv_kernel(DiffProblem p)
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const bool one = t.lim[reg_row(i, g)] == 1;   // as in the dQ kernel
+                    const bool one = *lds_at<int>(t + kLim + 4 * reg_row(i, g)) == 1;   // as in the dQ kernel
                     s[0][i] = one ? 0.f : s[0][i];
                     s[1][i] = one ? 0.f : s[1][i];
                 }
@@ -229,18 +233,19 @@ diff_dkv_kernel(DiffProblem p)
                 const Frag<E> f = frag_of(pd, h, E());
 #pragma unroll
                 for (int i = 0; i < DV / 32; ++i)
-                    gv[i] = mma(col_frag<E, DV>(t.go, h, 32 * i), f, gv[i]);
+                    gv[i] = mma(col_frag<E, DV>(gcol, h, i), f, gv[i]);
 #pragma unroll
                 for (int a = 0; a < 2; ++a) {
                     const Frag<E> ds = frag_of(s[a], h, E());
 #pragma unroll
                     for (int i = 0; i < DK / 32; ++i)
-                        gk[a][i] = mma(col_frag<E, DK>(t.q[a], h, 32 * i), ds, gk[a][i]);
+                        gk[a][i] = mma(col_frag<E, DK>(qcol + a * kMap, h, i), ds, gk[a][i]);
                 }
             }
         }
         if (r1 < rend)
-            commit(r1, buf[at_buf ^ 1]);
+            commit(r1, other);
+        exchange(t, other);
         r0 = r1;
     }
     if (key >= p.nk)
@@ -399,8 +404,6 @@ hipError_t launch_diff_backward(DiffProblem p, void *workspace, hipStream_t s)
         return hipGetLastError();
     }
     set_common(&p);
-    p.vec_go = view_vec(p.go, p.dv, e);
-    p.vec_o = view_vec(p.o, p.dv, e);
     p.vec_gq = store_vec(p.gq, p.d, e);
     p.vec_gk = store_vec(p.gk, p.d, e);
     p.vec_gv = store_vec(p.gv, p.dv, e);

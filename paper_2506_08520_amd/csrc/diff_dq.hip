@@ -1,5 +1,6 @@
 // Backward pass of differential attention, first half: dQ, row by row (the formulas stand
 // in diff_common.hpp).
+
 #include "diff_common.hpp"
 
 namespace nystra {
@@ -30,7 +31,8 @@ diff_dq_kernel(DiffProblem p)
     using T = typename E::T;
     using Tiles = KeyTiles<E, DK, DV, 64 * NW, DIRECT>;
     constexpr int KT = Tiles::KT;
-    __shared__ typename Tiles::Buffer buf[2];
+    __shared__ alignas(256) char lds[2 * Tiles::kBuffer];
+    const uint32_t buf = lds_offset(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
     const int64_t b = xcd_order(blockIdx.x, gridDim.x);
     const int tile = int(b % p.tiles);
@@ -49,7 +51,7 @@ diff_dq_kernel(DiffProblem p)
 
     Tiles tiles;
     if (kend > 0)
-        tiles.fetch(p, k0, v0, 0, kend, buf[0]);
+        tiles.fetch(p, k0, v0, 0, kend, buf);
     Frag<E> q[2][DK / 16], go[DV / 16];
     float L[2], D[2] = {0.f, 0.f};
 #pragma unroll
@@ -58,7 +60,7 @@ diff_dq_kernel(DiffProblem p)
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
             q[a][i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
-                                                       p.d - 16 * i - 8 * g, live, p.vec_q));
+                                                       p.d - 16 * i - 8 * g, live, p.d));
         L[a] = limit > 0 ? p.lse[(int64_t(w) * 2 * p.H + 2 * row.head + a) * p.nq + row.token]
                          : INFINITY;   // exp2(-inf) = 0 where no key is seen
     }
@@ -66,49 +68,49 @@ diff_dq_kernel(DiffProblem p)
 #pragma unroll
     for (int i = 0; i < DV / 16; ++i)
         go[i] = as_frag<E>(load_chunk<E, DIRECT>(gosrc + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
-                                                 live, p.vec_go));
+                                                 live, p.dv));
     if constexpr (KEPT) {
         const float *o2 = map_row<E>(p, w, row);
         const float *o1 = E::bytes == 2 ? o2 + p.dv : at<F32>(p.o, w, row.head, row.token);
-        const int vec2 = p.dv % 4 == 0 ? 16 : 4, vec1 = E::bytes == 2 ? vec2 : p.vec_o;
 #pragma unroll 2   // more would hold more of the rows at once than there are registers
         for (int col = 8 * g; col < p.dv; col += 16) {
             const int n = p.dv - col;
-            const Frag<E> x = as_frag<E>(load_chunk<E, DIRECT>(gosrc + col, n, live, p.vec_go));
-            D[0] += dot8(x, load_chunk<F32, false>(o1 + col, n, live, vec1));
-            D[1] += dot8(x, load_chunk<F32, false>(o2 + col, n, live, vec2));
+            const Frag<E> x = as_frag<E>(load_chunk<E, DIRECT>(gosrc + col, n, live, p.dv));
+            D[0] += dot8(x, load_chunk<F32, false>(o1 + col, n, live, p.dv));
+            D[1] += dot8(x, load_chunk<F32, false>(o2 + col, n, live, p.dv));
         }
         if (E::bytes == 4)
             D[0] = fmaf(lam, D[1], D[0]);
 #pragma unroll
         for (int a = 0; a < 2; ++a)
-            D[a] += other_half(D[a]);
+            D[a] = half_sum(D[a]);
     }
     f16v acc[2][DK / 32] = {};
     float glam = 0.f;
     if (kend > 0)
-        tiles.commit(buf[0]);
-    int at_buf = 0;
+        tiles.commit(buf);
+    uint32_t t = buf, other = buf + Tiles::kBuffer;   // this tile's buffer and the next one's
     for (int sweep = KEPT ? 1 : 0; sweep < 2; ++sweep) {
         float sum[2] = {0.f, 0.f};
-        for (int key = 0; key < kend; key += KT, at_buf ^= 1) {
+        for (int key = 0; key < kend; key += KT) {
             Tiles::ready();
             const bool wrap = key + KT >= kend, more = !wrap || sweep == 0;
             if (more)
-                tiles.fetch(p, k0, v0, wrap ? 0 : key + KT, kend, buf[at_buf ^ 1]);
-            const typename Tiles::Buffer &t = buf[at_buf];
+                tiles.fetch(p, k0, v0, wrap ? 0 : key + KT, kend, other);
             if (__any(key < limit)) {
+                const uint32_t krow = first_row<E, DK>(t), kcol = first_col<E, DK>(t);
+                const uint32_t vrow = first_row<E, DV>(t + Tiles::kV);
+                constexpr uint32_t kMap = KT * Tiles::LK::pitch;
                 f16v s[2] = {}, x = {};
 #pragma unroll
-                for (int a = 0; a < 2; ++a) {
+                for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
-                    for (int i = 0; i < DK / 16; ++i)
-                        s[a] = mma(row_frag<E, DK>(t.k[a], i), q[a][i], s[a]);
-                    part();
-                }
+                    for (int a = 0; a < 2; ++a)
+                        s[a] = mma(row_frag<E>(krow + a * kMap, i), q[a][i], s[a]);
+                part();
 #pragma unroll
                 for (int i = 0; i < DV / 16; ++i)
-                    x = mma(row_frag<E, DV>(t.v, i), go[i], x);
+                    x = mma(row_frag<E>(vrow, i), go[i], x);
                 part();
                 if (!__all(key + KT <= limit)) {
                     hide(s[0], limit, key, g);
@@ -139,20 +141,21 @@ diff_dq_kernel(DiffProblem p)
                             const Frag<E> ds = frag_of(s[a], h, E());
 #pragma unroll
                             for (int i = 0; i < DK / 32; ++i)
-                                acc[a][i] = mma(col_frag<E, DK>(t.k[a], h, 32 * i), ds, acc[a][i]);
+                                acc[a][i] = mma(col_frag<E, DK>(kcol + a * kMap, h, i), ds, acc[a][i]);
                         }
                 }
             }
             if (more)
-                tiles.commit(buf[at_buf ^ 1]);
+                tiles.commit(other);
+            exchange(t, other);
         }
         if (sweep == 0) {
 #pragma unroll
             for (int a = 0; a < 2; ++a)
-                D[a] = sum[a] + other_half(sum[a]);
+                D[a] = half_sum(sum[a]);
         }
     }
-    glam += other_half(glam);
+    glam = half_sum(glam);
     // What the dK, dV kernel needs of a row, also for those up to the end of the last tile
     // of 32.
     if (g == 0 && r < p.rows32)

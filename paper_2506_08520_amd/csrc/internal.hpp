@@ -148,7 +148,6 @@ struct DiffProblem {
 
     uint32_t nq_mul;       // division by nq
     int nq_shift;
-    int vec_q, vec_k, vec_v, vec_go, vec_o;
     bool store_o, vec_gq, vec_gk, vec_gv;
     int tiles, ktiles, splits, chunk, rsplits, rchunk, d4, dv4, partial_row;
     int64_t rows32;        // rows of a unit, up to a multiple of 32
