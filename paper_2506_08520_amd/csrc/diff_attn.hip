@@ -9,7 +9,7 @@ namespace {
 using namespace diff;
 
 constexpr int kMerge = 256;       // threads of the merge kernel: one row
-constexpr int kMaxSplits = 1024;
+constexpr int kFewSplits = 8;
 
 template <class E, int DK, int DV, int NW, bool DIRECT>
 __global__ void __launch_bounds__(64 * NW, (NW == 1 && !DIRECT ? 1 : occupancy<E, DV>()))
@@ -135,8 +135,9 @@ diff_forward_kernel(DiffProblem p)
                 y[j] = acc[1][i][4 * t + j] * inv2;
             }
             const int col = 32 * i + 8 * t + 4 * g;
-            store4<E>(o, col, p.dv, p.store_o, x[0] - lam * y[0], x[1] - lam * y[1],
-                      x[2] - lam * y[2], x[3] - lam * y[3]);
+            store4<E>(o, col, p.dv, p.store_o, difference(x[0], lam, y[0]),
+                      difference(x[1], lam, y[1]), difference(x[2], lam, y[2]),
+                      difference(x[3], lam, y[3]));
             if (maps) {
                 store4<F32>(maps, col, p.dv, p.dv % 4 == 0, y[0], y[1], y[2], y[3]);
                 if (E::bytes == 2)
@@ -150,13 +151,71 @@ diff_forward_kernel(DiffProblem p)
     }
 }
 
-// Joins the key ranges of one row: the weights of the ranges first, then the columns of
-// both maps, a thread to a column.
+// Joins few key ranges, a thread to four columns of a row: each forms the weights itself.
+template <class E>
+__global__ void __launch_bounds__(kMerge)
+diff_merge_few_kernel(DiffProblem p, int64_t items)
+{
+    const int64_t item = int64_t(blockIdx.x) * kMerge + threadIdx.x;
+    if (item >= items)
+        return;
+    const int nrows = p.R * p.nq, groups = p.dv4 / 4;
+    const int64_t at_row = item / groups;
+    const int col = int(item - at_row * groups) * 4;
+    const int64_t unit = at_row / nrows;
+    const int r = int(at_row - unit * nrows);
+    const int w = int(unit / p.G), kvh = int(unit % p.G);
+    const Row row = row_of(p, kvh, r);
+    const float *part = p.partial + (unit * p.splits * nrows + r) * p.partial_row;
+    const int64_t step = int64_t(nrows) * p.partial_row;
+    f4 ml[kFewSplits];
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {
+        const f4 none = {-INFINITY, 0.f, -INFINITY, 0.f};
+        ml[s] = s < p.splits ? *reinterpret_cast<const f4 *>(part + s * step + 2 * p.dv4) : none;
+        m[0] = fmaxf(m[0], ml[s][0]);
+        m[1] = fmaxf(m[1], ml[s][2]);
+    }
+    f4 x[2] = {};
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s)
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            if (ml[s][2 * a] != -INFINITY) {
+                const float e = fast_exp2(ml[s][2 * a] - m[a]);
+                l[a] = fmaf(e, ml[s][2 * a + 1], l[a]);
+                x[a] += e * *reinterpret_cast<const f4 *>(part + s * step + a * p.dv4 + col);
+            }
+        }
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+        x[a] *= l[a] == 0.f ? 0.f : 1.f / l[a];
+    const float lam = p.lambda[row.head];
+    store4<E>(at_out<E>(p.o, w, row.head, row.token), col, p.dv, p.store_o,
+              difference(x[0][0], lam, x[1][0]), difference(x[0][1], lam, x[1][1]),
+              difference(x[0][2], lam, x[1][2]), difference(x[0][3], lam, x[1][3]));
+    if (p.maps) {
+        float *maps = map_row<E>(p, w, row);
+        store4<F32>(maps, col, p.dv, p.dv % 4 == 0, x[1][0], x[1][1], x[1][2], x[1][3]);
+        if (E::bytes == 2)
+            store4<F32>(maps + p.dv, col, p.dv, p.dv % 4 == 0, x[0][0], x[0][1], x[0][2], x[0][3]);
+    }
+    if (p.lse && col == 0) {
+        float *lse = p.lse + (int64_t(w) * 2 * p.H + 2 * row.head) * p.nq + row.token;
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+            lse[a * p.nq] = l[a] == 0.f ? -INFINITY : m[a] + log2f(l[a]);
+    }
+}
+
+// Joins the key ranges of one row, a thread to a column of either map: as the softmax
+// itself, one pass with a running maximum, kBatch ranges' values in flight at a time.
 template <class E>
 __global__ void __launch_bounds__(kMerge)
 diff_merge_kernel(DiffProblem p)
 {
-    __shared__ float weight[2][kMaxSplits];
+    constexpr int kBatch = 16;
     __shared__ float out[2][128];
     const int nrows = p.R * p.nq;
     const int64_t unit = blockIdx.x / unsigned(nrows);
@@ -165,45 +224,49 @@ diff_merge_kernel(DiffProblem p)
     const Row row = row_of(p, kvh, r);
     const float *part = p.partial + (unit * p.splits * nrows + r) * p.partial_row;
     const int64_t step = int64_t(nrows) * p.partial_row;
-    const int lane = threadIdx.x & 63, map = threadIdx.x >> 6;
-    if (map < 2) {   // one wave to each map's weights
-        const float *ml = part + 2 * p.dv4 + 2 * map;
-        float m = -INFINITY, l = 0.f;
-        for (int s = lane; s < p.splits; s += 64)
-            m = fmaxf(m, ml[s * step]);
-        m = wave_max(m);
-        const float base = m == -INFINITY ? 0.f : m;
-        for (int s = lane; s < p.splits; s += 64) {
-            const float e = fast_exp2(ml[s * step] - base);
-            l = fmaf(e, ml[s * step + 1], l);
-            weight[map][s] = e;
+    const int i = threadIdx.x, a = i >= p.dv4;   // 2 dv4 <= kMerge columns
+    if (i < 2 * p.dv4) {
+        const float *ml = part + 2 * p.dv4 + 2 * a;
+        float m = -INFINITY, l = 0.f, x = 0.f;
+        for (int s0 = 0; s0 < p.splits; s0 += kBatch) {
+            float mb[kBatch], lb[kBatch], xb[kBatch];
+            float mn = m;
+#pragma unroll
+            for (int s = 0; s < kBatch; ++s) {
+                const int64_t at = min(s0 + s, p.splits - 1) * step;
+                mb[s] = ml[at];
+                lb[s] = ml[at + 1];
+                xb[s] = part[at + i];
+            }
+#pragma unroll
+            for (int s = 0; s < kBatch; ++s)
+                mn = fmaxf(mn, mb[s]);
+            if (mn == -INFINITY)
+                continue;   // ranges without a key
+            const float alpha = fast_exp2(m - mn);
+            l *= alpha;
+            x *= alpha;
+            m = mn;
+#pragma unroll
+            for (int s = 0; s < kBatch; ++s) {
+                if (s0 + s < p.splits && mb[s] != -INFINITY) {
+                    const float e = fast_exp2(mb[s] - m);
+                    l = fmaf(e, lb[s], l);
+                    x = fmaf(e, xb[s], x);
+                }
+            }
         }
-        l = wave_sum(l);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        for (int s = lane; s < p.splits; s += 64)
-            weight[map][s] *= inv;
-        if (p.lse && lane == 0)
-            p.lse[(int64_t(w) * 2 * p.H + 2 * row.head + map) * p.nq + row.token] =
+        out[a][i - a * p.dv4] = l == 0.f ? 0.f : x / l;
+        if (p.lse && i == a * p.dv4)
+            p.lse[(int64_t(w) * 2 * p.H + 2 * row.head + a) * p.nq + row.token] =
                 l == 0.f ? -INFINITY : m + log2f(l);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * p.dv4; i += kMerge) {
-        const int a = i >= p.dv4;
-        float x = 0.f;
-#pragma unroll 8
-        for (int s = 0; s < p.splits; ++s) {
-            const float e = weight[a][s];   // 0: the range may hold no sums
-            const float y = part[s * step + i];
-            x = e != 0.f ? fmaf(e, y, x) : x;
-        }
-        out[a][i - a * p.dv4] = x;
     }
     __syncthreads();
     const float lam = p.lambda[row.head];
     typename E::T *o = at_out<E>(p.o, w, row.head, row.token);
     float *maps = p.maps ? map_row<E>(p, w, row) : nullptr;
     for (int col = threadIdx.x; col < p.dv; col += kMerge) {
-        E::store(o, col, out[0][col] - lam * out[1][col]);
+        E::store(o, col, difference(out[0][col], lam, out[1][col]));
         if (maps) {
             maps[col] = out[1][col];
             if (E::bytes == 2)
@@ -219,8 +282,10 @@ struct Plan {
     int64_t blocks;
 };
 
-// Key ranges: with few rows enough of them for eight waves on each of the 256 CUs, of
-// at least two tiles each; a single wave's rows may be split finer than a workgroup's.
+// Key ranges: with few rows enough of them for eight waves on each of the 256 CUs, of at
+// least one tile to a wave.  Workgroups of more waves are split only below one to a CU: 5 x 25
+// of them over 777 keys (fp32, causal) took 196 us in one range and in three, and joining
+// the three another 72 us.
 Plan forward_plan(const DiffProblem &p)
 {
     Plan f;
@@ -228,8 +293,9 @@ Plan forward_plan(const DiffProblem &p)
     f.waves = waves_for(rows);
     f.tiles = ceil_div(rows, 32 * f.waves);
     const int64_t blocks = int64_t(p.W) * p.G * f.tiles;
-    const int64_t want = (2048 / f.waves + blocks - 1) / blocks;
-    const int64_t most = std::min<int64_t>(ceil_div(p.nk, 64 * f.waves), kMaxSplits);
+    const int64_t want = std::max<int64_t>(f.waves == 1 ? (2048 + blocks - 1) / blocks
+                                                        : 1024 / f.waves / blocks, 1);
+    const int64_t most = ceil_div(p.nk, 32 * f.waves);
     f.splits = int(std::min(want, most));
     f.chunk = ceil_div(ceil_div(p.nk, f.splits), 32) * 32;
     f.splits = ceil_div(p.nk, f.chunk);
@@ -303,7 +369,17 @@ hipError_t launch_diff_forward(DiffProblem p, void *workspace, hipStream_t s)
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess || f.splits == 1)
         return err;
-    const dim3 grid(unsigned(int64_t(p.W) * p.G * p.R * p.nq));
+    const int64_t rows = int64_t(p.W) * p.G * p.R * p.nq;
+    if (f.splits <= kFewSplits) {
+        const int64_t items = rows * (p.dv4 / 4);
+        const dim3 grid(unsigned((items + kMerge - 1) / kMerge));
+        if (p.dtype == 0)
+            diff_merge_few_kernel<F32><<<grid, kMerge, 0, s>>>(p, items);
+        else
+            diff_merge_few_kernel<BF16><<<grid, kMerge, 0, s>>>(p, items);
+        return hipGetLastError();
+    }
+    const dim3 grid{unsigned(rows)};
     if (p.dtype == 0)
         diff_merge_kernel<F32><<<grid, kMerge, 0, s>>>(p);
     else

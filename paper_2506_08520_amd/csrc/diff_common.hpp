@@ -464,6 +464,14 @@ __device__ inline float *map_row(const DiffProblem &p, int w, const Row &row)
                         (E::bytes == 2 ? 2 * p.dv : p.dv);
 }
 
+// O from the two maps' outputs.  The difference is not fused with a product that gave its
+// terms, so that equal maps cancel exactly.
+__device__ inline float difference(float x, float lam, float y)
+{
+#pragma clang fp contract(off)
+    return x - lam * y;
+}
+
 // The transposed tile's register r: its row.
 __device__ inline int reg_row(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
 

@@ -39,6 +39,13 @@ __device__ inline void sum_dlam(const DiffProblem &p, int h, float *out)
     }
 }
 
+// The factor of dK.  A softmax over one key is constant, as in the dQ kernel; with a causal
+// mask the rows that see one key are taken out one by one.
+__device__ inline float key_scale(const DiffProblem &p, int len)
+{
+    return p.causal == 0 && len == 1 ? 0.f : p.scale;
+}
+
 // dK and dV: a wave owns 32 keys and walks over the unit's rows, so that the heads
 // that share the keys are summed in registers.  Keys at or behind the window's
 // length get zeros.  With few workgroups the rows are split over p.rsplits of them, whose
@@ -139,13 +146,16 @@ diff_dkv_kernel(DiffProblem p)
             sgo.load([&](int i) { return go0 + go_row(r0 + i); },
                      [&](int i) { return r0 + i < nrows; }, p.dv);
         }
-        if (threadIdx.x < QT) {
-            const float4 *stats = p.row_stats + unit * p.rows32 + r0;
-            if constexpr (DIRECT)
+        const float4 *stats = p.row_stats + unit * p.rows32 + r0;
+        const float *lams = p.row_lambda + unit * p.rows32 + r0;
+        if constexpr (DIRECT) {
+            if (threadIdx.x < QT)
                 load_to_lds(stats, 16 * threadIdx.x, t + kStat);
-            else
-                sstat = *reinterpret_cast<const f4 *>(stats + threadIdx.x);
-            slam = p.lambda[row_of(p, kvh, min(r0 + int(threadIdx.x), nrows - 1)).head];
+            if (threadIdx.x < QT / 4)
+                load_to_lds(lams, 16 * threadIdx.x, t + kLam);
+        } else if (threadIdx.x < QT) {
+            sstat = *reinterpret_cast<const f4 *>(stats + threadIdx.x);
+            slam = lams[threadIdx.x];
         }
     };
     auto commit = [&](int r0, uint32_t t) {
@@ -154,12 +164,15 @@ diff_dkv_kernel(DiffProblem p)
             sgo.store(t + kGo);
         }
         if (threadIdx.x < QT) {
-            const int r = r0 + threadIdx.x;
-            if constexpr (!DIRECT)
+            if constexpr (!DIRECT) {
                 *lds_at<f4>(t + kStat + 16 * threadIdx.x) = sstat;
-            *lds_at<float>(t + kLam + 4 * threadIdx.x) = slam;
-            *lds_at<int>(t + kLim + 4 * threadIdx.x) =
-                r < nrows ? key_limit(p, len, row_of(p, kvh, r).token) : 0;
+                *lds_at<float>(t + kLam + 4 * threadIdx.x) = slam;
+            }
+            if (p.causal) {
+                const int r = r0 + threadIdx.x;
+                *lds_at<int>(t + kLim + 4 * threadIdx.x) =
+                    r < nrows ? key_limit(p, len, row_of(p, kvh, r).token) : 0;
+            }
         }
     };
     int r0 = kb < len ? next(split * p.rchunk) : rend;
@@ -173,14 +186,14 @@ diff_dkv_kernel(DiffProblem p)
             arrived();
         __syncthreads();
         const int r1 = next(r0 + QT);
-        if (r1 < rend)
-            fetch(r1, other);
-        const int rowlim = *lds_at<int>(t + kLim + 4 * c);
-        if (__any(kw < rowlim)) {
-            const bool masked = !__all(kw + 32 <= rowlim);
-            const uint32_t qrow = first_row<E, DK>(t), qcol = first_col<E, DK>(t);
-            const uint32_t grow = first_row<E, DV>(t + kGo), gcol = first_col<E, DV>(t + kGo);
-            f16v s[2] = {}, x = {};
+        // Without a causal mask every row sees every key there is, and rows behind the last
+        // have probabilities of zero.
+        const int rowlim = p.causal ? *lds_at<int>(t + kLim + 4 * c) : len;
+        const bool any = __any(kw < rowlim), masked = p.causal && !__all(kw + 32 <= rowlim);
+        f16v s[2] = {}, x = {};
+        if (any) {
+            const uint32_t qrow = first_row<E, DK>(t);
+            const uint32_t grow = first_row<E, DV>(t + kGo);
 #pragma unroll
             for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
@@ -196,6 +209,13 @@ diff_dkv_kernel(DiffProblem p)
                     x = mma(row_frag<E>(grow, i), v[i], x);
             }
             part();
+        }
+        // The next tile's loads, behind the first products: a register that the compiler
+        // keeps in memory is waited for with all loads before it.
+        if (r1 < rend)
+            fetch(r1, other);
+        if (any) {
+            const uint32_t qcol = first_col<E, DK>(t), gcol = first_col<E, DV>(t + kGo);
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -269,6 +289,7 @@ diff_dkv_kernel(DiffProblem p)
                             gv[i][4 * j + 1], gv[i][4 * j + 2], gv[i][4 * j + 3]);
         return;
     }
+    const float scale = key_scale(p, len);
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
         T *dst = at_out<E>(p.gk, w, 2 * kvh + a, key);
@@ -277,10 +298,10 @@ diff_dkv_kernel(DiffProblem p)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 store4<E>(dst, 32 * i + 8 * j + 4 * g, p.d, p.vec_gk,
-                          live ? p.scale * gk[a][i][4 * j] : 0.f,
-                          live ? p.scale * gk[a][i][4 * j + 1] : 0.f,
-                          live ? p.scale * gk[a][i][4 * j + 2] : 0.f,
-                          live ? p.scale * gk[a][i][4 * j + 3] : 0.f);
+                          live ? scale * gk[a][i][4 * j] : 0.f,
+                          live ? scale * gk[a][i][4 * j + 1] : 0.f,
+                          live ? scale * gk[a][i][4 * j + 2] : 0.f,
+                          live ? scale * gk[a][i][4 * j + 3] : 0.f);
     }
     T *dst = at_out<E>(p.gv, w, kvh, key);
 #pragma unroll
@@ -300,7 +321,9 @@ diff_dkv_merge_kernel(DiffProblem p)
     const int64_t unit = blockIdx.x / unsigned(p.nk);
     const int key = int(blockIdx.x - unit * p.nk);
     const int w = int(unit / p.G), kvh = int(unit % p.G);
-    const bool live = key < window_len(p, w);
+    const int len = window_len(p, w);
+    const bool live = key < len;
+    const float scale = key_scale(p, len);
     const float *part = p.partial + (unit * p.rsplits * p.nk + key) * p.partial_row;
     const int64_t step = int64_t(p.nk) * p.partial_row;
     for (int col = threadIdx.x; col < 2 * p.d4 + p.dv4; col += kMerge) {
@@ -311,7 +334,7 @@ diff_dkv_merge_kernel(DiffProblem p)
         if (col < 2 * p.d4) {
             const int a = col >= p.d4, at_col = col - a * p.d4;
             if (at_col < p.d)
-                E::store(at_out<E>(p.gk, w, 2 * kvh + a, key), at_col, p.scale * s);
+                E::store(at_out<E>(p.gk, w, 2 * kvh + a, key), at_col, scale * s);
         } else if (col - 2 * p.d4 < p.dv) {
             E::store(at_out<E>(p.gv, w, kvh, key), col - 2 * p.d4, s);
         }
@@ -374,15 +397,17 @@ void plan_rows(DiffProblem *p, int waves)
     p->partial_row = 2 * p->d4 + p->dv4;
 }
 
-// The workspace's parts: a record of each row, dlam's rows, and dK and dV by row range.
+// The workspace's parts: a record of each row and its lambda, dlam's rows, and dK and dV by
+// row range.
 struct Parts {
-    int64_t stats, lam, partial;
+    int64_t stats, lambda, lam, partial;
 };
 
 Parts parts_of(const DiffProblem &p)
 {
     const int64_t units = int64_t(p.W) * p.G;
-    return Parts{round256(units * p.rows32 * 16), round256(int64_t(p.W) * p.H * p.nq * 4),
+    return Parts{round256(units * p.rows32 * 16), round256(units * p.rows32 * 4),
+                 round256(int64_t(p.W) * p.H * p.nq * 4),
                  p.rsplits > 1 ? units * p.rsplits * p.nk * p.partial_row * 4 : 0};
 }
 
@@ -393,7 +418,7 @@ size_t diff_backward_workspace(const DiffProblem &p)
     DiffProblem t = p;
     plan_rows(&t, backward_waves(p.nk));
     const Parts b = parts_of(t);
-    return size_t(b.stats + b.lam + b.partial);
+    return size_t(b.stats + b.lambda + b.lam + b.partial);
 }
 
 hipError_t launch_diff_backward(DiffProblem p, void *workspace, hipStream_t s)
@@ -414,8 +439,9 @@ hipError_t launch_diff_backward(DiffProblem p, void *workspace, hipStream_t s)
     const Parts b = parts_of(p);
     char *ws = static_cast<char *>(workspace);
     p.row_stats = reinterpret_cast<float4 *>(ws);
-    p.rows_lam = reinterpret_cast<float *>(ws + b.stats);
-    p.partial = reinterpret_cast<float *>(ws + b.stats + b.lam);
+    p.row_lambda = reinterpret_cast<float *>(ws + b.stats);
+    p.rows_lam = reinterpret_cast<float *>(ws + b.stats + b.lambda);
+    p.partial = reinterpret_cast<float *>(ws + b.stats + b.lambda + b.lam);
     hipError_t err = launch_diff_dq(p, wq, units * p.tiles, s);
     if (err != hipSuccess)
         return err;

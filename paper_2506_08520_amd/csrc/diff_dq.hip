@@ -158,9 +158,11 @@ diff_dq_kernel(DiffProblem p)
     glam = half_sum(glam);
     // What the dK, dV kernel needs of a row, also for those up to the end of the last tile
     // of 32.
-    if (g == 0 && r < p.rows32)
+    if (g == 0 && r < p.rows32) {
         p.row_stats[unit * p.rows32 + r] = limit > 0 ? make_float4(L[0], L[1], D[0], D[1])
                                                      : make_float4(L[0], L[1], 0.f, 0.f);
+        p.row_lambda[unit * p.rows32 + r] = lam;
+    }
     if (!live)
         return;
     if (g == 0)

@@ -82,9 +82,11 @@ dropout_kernel(DropProblem p)
                     const T re = rv[h][j];
                     base = E::load(&re, 0);
                 }
-                T ye;
-                E::store(&ye, 0, res ? base + kept : kept);
-                out[j] = ye;
+                const float sum = res ? base + kept : kept;
+                if constexpr (E::bytes == 4)
+                    out[j] = sum;
+                else
+                    out[j] = __builtin_bit_cast(uint16_t, __bf16(sum));   // to nearest even
             }
             reinterpret_cast<V *>(y)[h] = out;
         }

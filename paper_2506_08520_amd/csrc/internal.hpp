@@ -151,7 +151,7 @@ struct DiffProblem {
     bool store_o, vec_gq, vec_gk, vec_gv;
     int tiles, ktiles, splits, chunk, rsplits, rchunk, d4, dv4, partial_row;
     int64_t rows32;        // rows of a unit, up to a multiple of 32
-    float *partial, *rows_lam;
+    float *partial, *rows_lam, *row_lambda;   // [units][rows32] the last
     float4 *row_stats;     // [units][rows32]: L_1, L_2, D_1, D_2
 };
 // Whether the grids of a call stay under the limits of a launch.

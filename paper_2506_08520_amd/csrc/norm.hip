@@ -17,29 +17,52 @@
 // launch adds them up, always in the same order (no atomics).
 #include "device_common.hpp"
 #include "internal.hpp"
+#include "tile_common.hpp"
 
 namespace nystra {
 namespace {
 
 constexpr int kThreads = 256;
 
-// VEC consecutive elements; the address is aligned to all of them.
+// VEC consecutive elements as they lie in memory; the address is aligned to all of them.
+template <class E, int VEC>
+struct Raw {
+    typedef typename E::T V __attribute__((ext_vector_type(VEC)));
+    V v;
+};
+
+template <class E>
+struct Raw<E, 1> {
+    typename E::T v;
+};
+
+template <class E, int VEC>
+__device__ inline Raw<E, VEC> load_raw(const typename E::T *p)
+{
+    return Raw<E, VEC>{*reinterpret_cast<const decltype(Raw<E, VEC>::v) *>(p)};
+}
+
+template <class E, int VEC>
+__device__ inline void unpack(const Raw<E, VEC> &r, float (&x)[VEC])
+{
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        typename E::T e;
+        if constexpr (VEC == 1)
+            e = r.v;
+        else
+            e = r.v[j];
+        if constexpr (E::bytes == 4)
+            x[j] = e;
+        else
+            x[j] = bf16_to_f32(e);
+    }
+}
+
 template <class E, int VEC>
 __device__ inline void load_vec(const typename E::T *p, float (&x)[VEC])
 {
-    typedef typename E::T V __attribute__((ext_vector_type(VEC)));
-    if constexpr (VEC == 1) {
-        x[0] = E::load(p, 0);
-    } else {
-        const V v = *reinterpret_cast<const V *>(p);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            if constexpr (E::bytes == 4)
-                x[j] = v[j];
-            else
-                x[j] = bf16_to_f32(v[j]);
-        }
-    }
+    unpack<E, VEC>(load_raw<E, VEC>(p), x);
 }
 
 template <class E, int VEC>
@@ -49,27 +72,35 @@ __device__ inline void store_vec(typename E::T *p, const float (&x)[VEC])
     if constexpr (VEC == 1) {
         E::store(p, 0, x[0]);
     } else {
-        V v;
+        if constexpr (E::bytes == 4) {
+            V v;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            if constexpr (E::bytes == 4)
+            for (int j = 0; j < VEC; ++j)
                 v[j] = x[j];
-            else
-                v[j] = f32_to_bf16(x[j]);
+            *reinterpret_cast<V *>(p) = v;
+        } else {
+            typedef float FV __attribute__((ext_vector_type(VEC)));
+            typedef __bf16 BV __attribute__((ext_vector_type(VEC)));
+            FV v;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                v[j] = x[j];
+            *reinterpret_cast<BV *>(p) = __builtin_convertvector(v, BV);   // to nearest even
         }
-        *reinterpret_cast<V *>(p) = v;
     }
 }
 
-// Sums over the LPR lanes of a row.  Rows of a whole workgroup go through LDS.
+// Sums over the LPR lanes of a row, by lane exchanges inside the VALU.  Rows of a whole
+// workgroup go through LDS.
 template <int LPR, int N>
 __device__ inline void row_sums(float (&s)[N], float *lds)
 {
 #pragma unroll
-    for (int o = (LPR < 64 ? LPR : 64) / 2; o >= 1; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            s[i] += __shfl_xor(s[i], o, 64);
+    for (int i = 0; i < N; ++i) {
+        s[i] = tile::sum_row(s[i]);
+        if constexpr (LPR >= 64)
+            s[i] = tile::sum_groups(s[i]);
+    }
     if constexpr (LPR > 64) {
         constexpr int W = LPR / 64;
         const int wave = threadIdx.x >> 6;
@@ -183,29 +214,47 @@ norm_backward_kernel(NormProblem p, float *partial)
         if (p.w && col < p.C)
             load_vec<E, VEC>(static_cast<const T *>(p.w) + col, w[c]);
     }
-    for (int64_t r0 = int64_t(blockIdx.x) * kRows; r0 < p.rows; r0 += int64_t(gridDim.x) * kRows) {
-        const int64_t row = r0 + group;
-        const bool live = row < p.rows;
-        const int64_t rr = live ? row : r0;
+    // The rows are fetched one ahead: with few rows to a workgroup it is the latency of
+    // their loads that bounds it.
+    const int64_t step = int64_t(gridDim.x) * kRows;
+    int64_t row = int64_t(blockIdx.x) * kRows + group;
+    Raw<E, VEC> xn[CH], gn[CH];
+    float mean_n = 0.f, rstd_n = 0.f;
+    auto fetch = [&](int64_t r) {
+        const int64_t rr = r < p.rows ? r : 0;
         const T *x = static_cast<const T *>(p.x) + rr * p.x_stride;
         const T *dy = static_cast<const T *>(p.dy) + rr * p.dy_stride;
-        const float mean = p.mean[rr], rstd = p.rstd[rr];
-        float xh[CH][VEC], g[CH][VEC];
-        float s[2] = {0.f, 0.f};
+        mean_n = p.mean[rr];
+        rstd_n = p.rstd[rr];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
+            // Lanes behind the row load its start again, and drop it below.
             const int col = (c * LPR + lane) * VEC;
-            if (live && col < p.C) {
-                load_vec<E, VEC>(x + col, xh[c]);
-                load_vec<E, VEC>(dy + col, g[c]);
+            xn[c] = load_raw<E, VEC>(x + (col < p.C ? col : 0));
+            gn[c] = load_raw<E, VEC>(dy + (col < p.C ? col : 0));
+        }
+    };
+    fetch(row);
+    for (int64_t r0 = int64_t(blockIdx.x) * kRows; r0 < p.rows; r0 += step, row += step) {
+        const bool live = row < p.rows;
+        const float mean = mean_n, rstd = rstd_n;
+        float xh[CH][VEC], g[CH][VEC];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    xh[c][j] = (xh[c][j] - mean) * rstd;
-            } else {
+        for (int c = 0; c < CH; ++c) {
+            const bool in = live && (c * LPR + lane) * VEC < p.C;
+            unpack<E, VEC>(xn[c], xh[c]);
+            unpack<E, VEC>(gn[c], g[c]);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    xh[c][j] = g[c][j] = 0.f;
+            for (int j = 0; j < VEC; ++j) {
+                xh[c][j] = in ? (xh[c][j] - mean) * rstd : 0.f;
+                g[c][j] = in ? g[c][j] : 0.f;
             }
+        }
+        if (r0 + step < p.rows)
+            fetch(row + step);
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 aw[c][j] = fmaf(g[c][j], xh[c][j], aw[c][j]);
@@ -214,7 +263,6 @@ norm_backward_kernel(NormProblem p, float *partial)
                 s[0] += g[c][j];
                 s[1] = fmaf(g[c][j], xh[c][j], s[1]);
             }
-        }
         row_sums<LPR>(s, lds);
         const float m0 = s[0] / float(p.C), m1 = s[1] / float(p.C);
         if (live) {
@@ -274,24 +322,31 @@ norm_backward_kernel(NormProblem p, float *partial)
     }
 }
 
-// Column sums of partial[n][2C]: 8 columns and 32 partials at a time to a workgroup.
+// Column sums of partial[n][2C]: eight columns to a workgroup, whose threads take every
+// 128th partial sum.
+constexpr int kReduce = 1024;
+
 template <class E>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kReduce)
 norm_reduce_kernel(const float *__restrict__ partial, int n, int C, typename E::T *dw,
                    typename E::T *db)
 {
-    __shared__ float lds[32][9];
+    __shared__ float lds[kReduce / 8][9];
     const int col = blockIdx.x * 8 + threadIdx.x % 8, part = threadIdx.x / 8;
     float s = 0.f;
-    if (col < 2 * C)
-        for (int i = part; i < n; i += 32)
+    if (col < 2 * C) {
+#pragma unroll 8
+        for (int i = part; i < n; i += kReduce / 8)
             s += partial[int64_t(i) * 2 * C + col];
+    }
     lds[part][threadIdx.x % 8] = s;
-    __syncthreads();
+    for (int half = kReduce / 16; half >= 1; half /= 2) {
+        __syncthreads();
+        if (part < half)
+            lds[part][threadIdx.x % 8] += lds[part + half][threadIdx.x % 8];
+    }
     if (part == 0 && col < 2 * C) {
-        s = 0.f;
-        for (int i = 0; i < 32; ++i)
-            s += lds[i][threadIdx.x];
+        s = lds[0][threadIdx.x];
         if (col < C) {
             if (dw)
                 E::store(dw, col, s);
@@ -399,10 +454,10 @@ hipError_t launch_norm_backward(const NormProblem &p, void *dw, void *db, float 
     if (dw || db) {
         const int blocks = (2 * p.C + 7) / 8;
         if (p.dtype == 0)
-            norm_reduce_kernel<F32><<<blocks, kThreads, 0, s>>>(
+            norm_reduce_kernel<F32><<<blocks, kReduce, 0, s>>>(
                 workspace, groups, p.C, static_cast<float *>(dw), static_cast<float *>(db));
         else
-            norm_reduce_kernel<BF16><<<blocks, kThreads, 0, s>>>(
+            norm_reduce_kernel<BF16><<<blocks, kReduce, 0, s>>>(
                 workspace, groups, p.C, static_cast<uint16_t *>(dw), static_cast<uint16_t *>(db));
     }
     return hipGetLastError();
