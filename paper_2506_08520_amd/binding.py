@@ -435,13 +435,14 @@ def _placed(f):
 
 def _raw_stream(t):
     import torch
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _same(first, tensors, dtype=None):
+    dtype, index = dtype or first.dtype, first.get_device()
     for t in tensors:
-        if t is not None and (t.device != first.device or t.dtype != (dtype or first.dtype)):
-            raise ValueError(f"expected {dtype or first.dtype} tensors on {first.device}")
+        if t is not None and (t.dtype != dtype or t.get_device() != index):
+            raise ValueError(f"expected {dtype} tensors on {first.device}")
 
 
 def _vector(t, n, what):
@@ -462,8 +463,17 @@ def _rows(t, C):
     return stride if t.numel() > C else C
 
 
+def _addr(t):
+    return t.data_ptr() if t is not None else None
+
+
 def _bytes(t):
     return t.numel() * t.element_size() if t is not None else 0
+
+
+def _contiguous_like(t):
+    import torch
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
 @_placed
@@ -471,26 +481,28 @@ def nystra_layer_norm_forward(x, weight=None, bias=None, eps=1e-5, with_stats=Fa
     """LayerNorm over the last dimension of x [..., C] (rows at one stride): y, or
     with_stats (y, mean, rstd) for the backward pass (fp32, one value to a row)."""
     import torch
-    C = int(x.shape[-1]) if x.dim() else 0
+    C = x.shape[-1] if x.dim() else 0
     code = _dtype_code(x)
     _same(x, (weight, bias, out))
     _vector(weight, C, "weight")
     _vector(bias, C, "bias")
     rows = x.numel() // max(C, 1)
-    if out is not None and out.shape != x.shape:
+    if out is None:
+        out = _contiguous_like(x)
+    elif out.shape != x.shape:
         raise ValueError("out must have x's shape")
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
     mean = rstd = None
     if with_stats:
-        mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-                      for _ in range(2))
-    rc = lib().nystra_layer_norm_forward(_ptr(x), _rows(x, C), _ptr(weight), _ptr(bias), _ptr(y),
-                                         _rows(y, C), _ptr(mean), _ptr(rstd), rows, C, eps, code,
-                                         _raw_stream(x))
+        mean, rstd = torch.empty((2,) + x.shape[:-1], dtype=torch.float32,
+                                 device=x.device).unbind(0)
+    rc = lib().nystra_layer_norm_forward(x.data_ptr(), _rows(x, C), _addr(weight), _addr(bias),
+                                         out.data_ptr(), _rows(out, C), _addr(mean), _addr(rstd),
+                                         rows, C, eps, code, _raw_stream(x))
     _check(rc, "nystra_layer_norm_forward")
-    return (y, mean, rstd) if with_stats else y
+    return (out, mean, rstd) if with_stats else out
 
 
+@functools.lru_cache(maxsize=256)
 def nystra_layer_norm_workspace_size(rows, channels):
     n = ctypes.c_size_t(0)
     _check(lib().nystra_layer_norm_workspace_size(rows, channels, ctypes.byref(n)),
@@ -502,7 +514,7 @@ def nystra_layer_norm_workspace_size(rows, channels):
 def nystra_layer_norm_backward(dy, x, weight, mean, rstd, workspace=None):
     """(dx, dweight, dbias) of nystra_layer_norm_forward; weight may be None (ones)."""
     import torch
-    C = int(x.shape[-1]) if x.dim() else 0
+    C = x.shape[-1] if x.dim() else 0
     code = _dtype_code(x)
     _same(dy, (x, weight))
     _same(dy, (mean, rstd), torch.float32)
@@ -512,16 +524,18 @@ def nystra_layer_norm_backward(dy, x, weight, mean, rstd, workspace=None):
     _vector(weight, C, "weight")
     _vector(mean, rows, "mean")
     _vector(rstd, rows, "rstd")
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dw, db = torch.empty(2, C, dtype=x.dtype, device=x.device).unbind(0)
+    dx = _contiguous_like(x)
+    dw, db = x.new_empty((2, C)).unbind(0)
     if workspace is None:
         workspace = torch.empty(nystra_layer_norm_workspace_size(rows, C), dtype=torch.uint8,
                                 device=x.device)
-    _same(dy, (workspace,), workspace.dtype)
-    rc = lib().nystra_layer_norm_backward(_ptr(dy), _rows(dy, C), _ptr(x), _rows(x, C),
-                                          _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx), C,
-                                          _ptr(dw), _ptr(db), rows, C, code, _ptr(workspace),
-                                          _bytes(workspace), _raw_stream(x))
+    else:
+        _same(dy, (workspace,), workspace.dtype)
+    rc = lib().nystra_layer_norm_backward(dy.data_ptr(), _rows(dy, C), x.data_ptr(), _rows(x, C),
+                                          _addr(weight), mean.data_ptr(), rstd.data_ptr(),
+                                          dx.data_ptr(), C, dw.data_ptr(), db.data_ptr(), rows, C,
+                                          code, workspace.data_ptr(), _bytes(workspace),
+                                          _raw_stream(x))
     _check(rc, "nystra_layer_norm_backward")
     return dx, dw, db
 
@@ -543,49 +557,64 @@ def nystra_dropout(x, p, seed=0, offset=0, state=None, residual=None, out=None):
         _vector(state, 2, "state")
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise ValueError("seed and offset must be in [0, 2^64)")
-    y = torch.empty_like(x) if out is None else out
-    rc = lib().nystra_dropout(_ptr(x), _ptr(residual), _ptr(y), x.numel(), p, seed, offset,
-                              _ptr(state), code, _raw_stream(x))
+    if out is None:
+        out = torch.empty_like(x)
+    rc = lib().nystra_dropout(x.data_ptr(), _addr(residual), out.data_ptr(), x.numel(), p, seed,
+                              offset, _addr(state), code, _raw_stream(x))
     _check(rc, "nystra_dropout")
-    return y
+    return out
 
 
 def _view(t):
-    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+    s = t.stride()
+    if len(s) != 4 or (s[3] != 1 and t.shape[3] > 1):
         raise ValueError("expected [windows, heads, tokens, width] with contiguous rows")
-    return View(t.data_ptr(), *t.stride()[:3])
+    return View(t.data_ptr(), s[0], s[1], s[2])
 
 
 def _diff_shape(q, k, v, lam, kv_len, scale, causal):
     import torch
-    for t in (q, k, v):
-        if t.dim() != 4:
-            raise ValueError("expected [windows, heads, tokens, width]")
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("expected [windows, heads, tokens, width]")
     _same(q, (k, v))
     _same(q, (lam,), torch.float32)
     W, H2, nq, d = q.shape
-    G, nk, dv = v.shape[1:]
-    if H2 % 2 != 0 or k.shape != (W, 2 * G, nk, d) or v.shape[0] != W:
+    Wv, G, nk, dv = v.shape
+    if H2 % 2 != 0 or k.shape != (W, 2 * G, nk, d) or Wv != W:
         raise ValueError("expected q [W, 2H, n_q, d], k [W, 2G, n_k, d] and v [W, G, n_k, d_v]")
     _vector(lam, H2 // 2, "lam")
     if kv_len is not None:
         _same(q, (kv_len,), torch.int32)
         _vector(kv_len, W, "kv_len")
-    return DiffShape(W, H2 // 2, G, nq, nk, d, dv, causal, scale)
+    return (W, H2 // 2, G, nq, nk, d, dv, causal, scale)
 
 
-def nystra_diff_attn_workspace_size(shape, backward=False, dtype=F32):
+@functools.lru_cache(maxsize=256)
+def _diff_workspace(shape, backward, dtype):
     n = ctypes.c_size_t(0)
-    _check(lib().nystra_diff_attn_workspace_size(ctypes.byref(shape), int(backward), dtype,
+    _check(lib().nystra_diff_attn_workspace_size(DiffShape(*shape), int(backward), dtype,
                                                  ctypes.byref(n)),
            "nystra_diff_attn_workspace_size")
     return int(n.value)
 
 
-def _kept(q, shape):
-    """What the backward pass needs of an output row: the second map's, and in bf16, whose
-    output is rounded, both."""
-    return (2, shape.d_v) if _dtype_code(q) == BF16 else (shape.d_v,)
+def nystra_diff_attn_workspace_size(shape, backward=False, dtype=F32):
+    """Bytes of workspace for a DiffShape (forward: 0 unless the keys are split)."""
+    return _diff_workspace(tuple(getattr(shape, n) for n, _ in DiffShape._fields_),
+                           bool(backward), dtype)
+
+
+def _diff_buffer(q, workspace, shape, backward, code):
+    """(tensor, address, bytes) of the caller's workspace, or of one made for the call."""
+    import torch
+    if workspace is not None:
+        _same(q, (workspace,), workspace.dtype)
+        return workspace, workspace.data_ptr(), _bytes(workspace)
+    need = _diff_workspace(shape, backward, code)
+    if need == 0:
+        return None, None, 0
+    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    return workspace, workspace.data_ptr(), need
 
 
 @_placed
@@ -600,27 +629,24 @@ def nystra_diff_attn_forward(q, k, v, lam, scale=0.0, causal=CAUSAL_NONE, kv_len
     import torch
     shape = _diff_shape(q, k, v, lam, kv_len, scale, causal)
     code = _dtype_code(q)
-    oshape = (shape.n_windows, shape.heads, shape.n_q, shape.d_v)
+    W, H, _, nq, nk, _, dv = shape[:7]
     if out is None:
-        out = torch.empty(oshape, dtype=q.dtype, device=q.device)
-    elif tuple(out.shape) != oshape:
-        raise ValueError(f"out must be {list(oshape)}")
-    _same(q, (out,))
+        out = q.new_empty((W, H, nq, dv))
+    else:
+        _same(q, (out,))
+        if out.shape != (W, H, nq, dv):
+            raise ValueError(f"out must be {[W, H, nq, dv]}")
     maps = lse = None
     if with_saved:
-        lse = torch.empty((shape.n_windows, 2 * shape.heads, shape.n_q), dtype=torch.float32,
-                          device=q.device)
-        if shape.n_k > DIFF_SHORT_KEYS:
-            maps = torch.empty(oshape[:3] + _kept(q, shape), dtype=torch.float32, device=q.device)
-    if workspace is None:
-        need = nystra_diff_attn_workspace_size(shape, False, code)
-        if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    else:
-        _same(q, (workspace,), workspace.dtype)
-    rc = lib().nystra_diff_attn_forward(_view(q), _view(k), _view(v), _ptr(lam), _ptr(kv_len),
-                                        _view(out), _ptr(maps), _ptr(lse), shape, code,
-                                        _ptr(workspace), _bytes(workspace), _raw_stream(q))
+        lse = torch.empty((W, 2 * H, nq), dtype=torch.float32, device=q.device)
+        if nk > DIFF_SHORT_KEYS:
+            # the second map's output, and in bf16, whose output is rounded, the first's
+            maps = torch.empty((W, H, nq) + ((2, dv) if code == BF16 else (dv,)),
+                               dtype=torch.float32, device=q.device)
+    workspace, ws, nbytes = _diff_buffer(q, workspace, shape, False, code)
+    rc = lib().nystra_diff_attn_forward(_view(q), _view(k), _view(v), lam.data_ptr(),
+                                        _addr(kv_len), _view(out), _addr(maps), _addr(lse),
+                                        DiffShape(*shape), code, ws, nbytes, _raw_stream(q))
     _check(rc, "nystra_diff_attn_forward")
     return (out, (maps, lse)) if with_saved else out
 
@@ -633,30 +659,26 @@ def nystra_diff_attn_backward(do, q, k, v, lam, o, saved, scale=0.0, causal=CAUS
     import torch
     shape = _diff_shape(q, k, v, lam, kv_len, scale, causal)
     code = _dtype_code(q)
+    W, H, _, nq, nk, _, dv = shape[:7]
     maps, lse = saved
-    oshape = (shape.n_windows, shape.heads, shape.n_q, shape.d_v)
-    if tuple(do.shape) != oshape or tuple(o.shape) != oshape:
-        raise ValueError(f"do and o must be {list(oshape)}")
+    if do.shape != (W, H, nq, dv) or o.shape != (W, H, nq, dv):
+        raise ValueError(f"do and o must be {[W, H, nq, dv]}")
     _same(do, (q, o))
     _same(do, (lse, maps), torch.float32)
-    _vector(maps, o.numel() * (2 if code == BF16 else 1), "saved maps")
-    _vector(lse, 2 * shape.n_windows * shape.heads * shape.n_q, "saved sums")
+    _vector(maps, o.numel() * (2 if code == BF16 else 1), "the saved maps")
+    _vector(lse, 2 * W * H * nq, "the saved sums")
     if grads is None:
-        grads = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-    dq, dk, dv = grads
-    for t, like in zip(grads, (q, k, v)):
-        if t.shape != like.shape:
-            raise ValueError("the gradients must have their inputs' shapes")
-    _same(do, grads)
-    dlam = torch.empty_like(lam)
-    if workspace is None:
-        need = nystra_diff_attn_workspace_size(shape, True, code)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        grads = tuple(t.new_empty(t.shape) for t in (q, k, v))
     else:
-        _same(do, (workspace,), workspace.dtype)
-    rc = lib().nystra_diff_attn_backward(_view(do), _view(q), _view(k), _view(v), _ptr(lam),
-                                         _ptr(kv_len), _view(o), _ptr(maps), _ptr(lse), _view(dq),
-                                         _view(dk), _view(dv), _ptr(dlam), shape, code,
-                                         _ptr(workspace), _bytes(workspace), _raw_stream(q))
+        _same(do, grads)
+        if any(t.shape != like.shape for t, like in zip(grads, (q, k, v))):
+            raise ValueError("the gradients must have their inputs' shapes")
+    dq, dk, dv_ = grads
+    dlam = torch.empty_like(lam)
+    workspace, ws, nbytes = _diff_buffer(q, workspace, shape, True, code)
+    rc = lib().nystra_diff_attn_backward(_view(do), _view(q), _view(k), _view(v), lam.data_ptr(),
+                                         _addr(kv_len), _view(o), _addr(maps), _addr(lse),
+                                         _view(dq), _view(dk), _view(dv_), dlam.data_ptr(),
+                                         DiffShape(*shape), code, ws, nbytes, _raw_stream(q))
     _check(rc, "nystra_diff_attn_backward")
-    return dq, dk, dv, dlam
+    return dq, dk, dv_, dlam

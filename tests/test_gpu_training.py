@@ -1,0 +1,166 @@
+"""The differentiable functions and the Transformer block that runs them together:
+gradients against a composition of torch operations in 64 bits, a training step, the
+refusal of recorded gradients."""
+import math
+
+import pytest
+import torch
+import torch.nn.functional as F
+
+from paper_2506_08520_amd import binding as B
+from paper_2506_08520_amd import training as T
+import operators_oracle as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def plain_block(block, x, seed, dtype, device):
+    """The block's arithmetic in torch operations, on copies of its parameters."""
+    P = {n: p.detach().to(device, dtype).requires_grad_() for n, p in block.named_parameters()}
+    x = x.detach().to(device, dtype).requires_grad_()
+    at, p = block.attn, block.p if block.training else 0.0
+    Bn, H, W, C = x.shape
+    w, h, s = at.window, at.heads, at.shift
+    d = C // (2 * h)
+
+    def norm(t, name, eps=1e-5):
+        return F.layer_norm(t, t.shape[-1:], P[name + ".weight"], P[name + ".bias"], eps)
+
+    def drop(t, offset):
+        if p == 0:
+            return t
+        keep = ref.keep_mask(t.numel(), p, seed, offset).reshape(t.shape).to(device)
+        thr = math.floor(p * 65536 + 0.5)
+        return torch.where(keep, t * (65536.0 / (65536 - thr)), torch.zeros_like(t))
+
+    t = norm(x, "norm1").roll((-s, -s), (1, 2))
+    t = t.reshape(Bn, H // w, w, W // w, w, C).transpose(2, 3).reshape(-1, w * w, C)
+    q, k, v = (t @ P["attn.qkv.weight"].t() + P["attn.qkv.bias"]).chunk(3, -1)
+    q, k = (u.unflatten(-1, (h, 2, d)).permute(0, 2, 3, 1, 4) for u in (q, k))
+    v = v.unflatten(-1, (h, 2 * d)).transpose(1, 2).contiguous()
+    m = torch.softmax(q @ k.transpose(-1, -2).contiguous() / math.sqrt(d), -1)
+    a1, b1, a2, b2 = P["attn.lam"]
+    lam = torch.exp((a1 * b1).sum(-1)) - torch.exp((a2 * b2).sum(-1)) + at.lam_init
+    o = (m[:, :, 0] - lam[:, None, None] * m[:, :, 1]) @ v
+    o = norm(o.transpose(1, 2), "attn.norm") * (1 - at.lam_init)
+    y = o.flatten(2) @ P["attn.proj.weight"].t() + P["attn.proj.bias"]
+    y = y.reshape(Bn, H // w, W // w, w, w, C).transpose(2, 3).reshape(Bn, H, W, C)
+    z = x + drop(y.roll((s, s), (1, 2)), 0)
+    u = F.gelu(norm(z, "norm2") @ P["mlp.0.weight"].t() + P["mlp.0.bias"])
+    z = z + drop(u @ P["mlp.2.weight"].t() + P["mlp.2.bias"], 1)
+    return x, P, z
+
+
+def rel(a, b):
+    return float((a.detach().double().cpu() - b).norm() / b.norm())
+
+
+@pytest.mark.parametrize("shape", [(1, 16, 24, 60, 3, 8, 4, 0.1), (2, 12, 12, 36, 2, 6, 0, 0.0),
+                                   (1, 24, 24, 64, 1, 12, 5, 0.5)], ids=str)
+def test_block_gradients(shape):
+    """fp32: output and every gradient are no further from 64 bits than four times what the
+    same composition of fp32 torch operations is (both round every step to fp32), or 2^-18: a
+    probability 2^(s - L) is off by about (|s| + |L|) 2^-24 of itself, 8 x 2^-24 at scores of a
+    few units, and the gradients of lam and of the biases are sums of both signs that keep
+    about an eighth of their terms' magnitude."""
+    Bn, H, W, C, heads, window, shift, p = shape
+    torch.manual_seed(1)
+    block = T.DifferentialTransformerBlock(C, heads, window, shift, p=p)
+    x = torch.randn(Bn, H, W, C, device="cuda", requires_grad=True)
+    g = torch.randn(Bn, H, W, C, device="cuda")
+    y = block(x, seed=77)
+    y.backward(g)
+    xr, P, yr = plain_block(block, x, 77, torch.float64, "cpu")
+    yr.backward(g.double().cpu())
+    xs, S, ys = plain_block(block, x, 77, torch.float32, "cpu")
+    ys.backward(g.cpu())
+    pairs = [("y", y, ys, yr), ("x", x.grad, xs.grad, xr.grad)]
+    pairs += [(n, q.grad, S[n].grad, P[n].grad) for n, q in block.named_parameters()]
+    for name, got, single, exact in pairs:
+        mine, theirs = rel(got, exact.detach()), rel(single, exact.detach())
+        print(f"{name}: {mine:.2e}, fp32 torch {theirs:.2e}")
+        assert mine <= max(4 * theirs, 2.0 ** -18), name
+
+
+def test_block_in_bf16_trains():
+    torch.manual_seed(2)
+    block = T.DifferentialTransformerBlock(180, 6, 8, 4, dtype=torch.bfloat16)
+    opt = torch.optim.SGD(block.parameters(), lr=1e-3)
+    x = torch.randn(1, 32, 32, 180, device="cuda").bfloat16()
+    for _ in range(3):
+        opt.zero_grad()
+        block(x).float().square().mean().backward()
+        for n, p in block.named_parameters():
+            assert p.grad is not None and torch.isfinite(p.grad).all(), n
+            assert p.grad.abs().max() > 0, n
+        opt.step()
+    block.eval()
+    with torch.no_grad():
+        assert torch.equal(block(x), block(x))
+
+
+def test_seeds_make_masks():
+    torch.manual_seed(3)
+    block = T.DifferentialTransformerBlock(36, 2, 6, p=0.5)
+    x = torch.randn(1, 12, 12, 36, device="cuda")
+    with torch.no_grad():
+        assert torch.equal(block(x, seed=5), block(x, seed=5))
+        assert not torch.equal(block(x, seed=5), block(x, seed=6))
+        torch.manual_seed(4)
+        a = block(x)
+        torch.manual_seed(4)
+        assert torch.equal(a, block(x)) and not torch.equal(a, block(x))
+
+
+def test_functions_pass_gradients_as_asked():
+    """Strided and expanded incoming gradients, inputs without gradient, a shared leaf."""
+    x = torch.randn(6, 40, device="cuda", requires_grad=True)
+    w = torch.randn(40, device="cuda", requires_grad=True)
+    T.layer_norm(x, w).sum().backward()                      # an expanded gradient
+    want = ref.layer_norm(x.detach().cpu(), w.detach().cpu(), None, 1e-5, torch.ones(6, 40))
+    ref.check(x.grad, want[1], "dx")
+    ref.check(w.grad, want[2], "dw")
+    y = torch.randn(40, 6, device="cuda", requires_grad=True)
+    keep = ref.keep_mask(240, 0.5, 9, 0).reshape(40, 6)
+    T.dropout(y, 0.5, 9, residual=y).t().square().sum().backward()
+    f = torch.where(keep, 3.0, 1.0).double()                 # y + 2 keep y, a leaf used twice
+    exact = 2 * (y.detach().cpu().double() * f) * f
+    assert (y.grad.cpu().double() - exact).abs().max() <= 8 * 2.0 ** -24 * exact.abs().max()
+    q, k, v = (torch.randn(2, n, 20, e, device="cuda") for n, e in ((4, 8), (4, 8), (2, 16)))
+    lam = torch.full((2,), 0.3, device="cuda", requires_grad=True)
+    v.requires_grad_()
+    o = T.differential_attention(q, k, v, lam)
+    do = torch.randn(2, 20, 2, 16, device="cuda").transpose(1, 2)
+    o.backward(do)
+    want = ref.diff_attention(q.cpu(), k.cpu(), v.detach().cpu(), lam.detach().cpu(), do=do.cpu())
+    ref.check(v.grad, want[3], "dv")
+    ref.check(lam.grad, want[4], "dlam")
+    assert q.grad is None
+
+
+def test_recorded_gradients_are_refused():
+    x = torch.randn(64, 40, device="cuda", requires_grad=True)
+    T.layer_norm(x)                                          # warm
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="recorded"):
+        with torch.cuda.graph(graph):
+            T.layer_norm(x)
+    torch.cuda.synchronize()
+    frozen = x.detach()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = T.dropout(T.layer_norm(frozen), 0.5, 3)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, T.dropout(T.layer_norm(frozen), 0.5, 3))
+
+
+def test_arguments():
+    for kw in (dict(dim=30, heads=4, window=8), dict(dim=32, heads=2, window=8, shift=8)):
+        with pytest.raises(ValueError):
+            T.DifferentialWindowAttention(**kw)
+    with pytest.raises(ValueError):
+        T.DifferentialTransformerBlock(32, 2, 8, p=1.5)
+    with pytest.raises(ValueError):
+        T.DifferentialWindowAttention(32, 2, 8)(torch.zeros(1, 12, 16, 32, device="cuda"))
