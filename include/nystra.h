@@ -381,15 +381,16 @@ int nystra_dropout(const void *X, const void *residual, void *Y, int64_t n, floa
  * cores; bf16 on the bf16 ones, with the probabilities (in the backward pass also the
  * gradients of the scores) rounded to bf16 for the products that take them.
  *
- * For training, lse (fp32 [n_windows][2 heads][n_q], base-2 logarithms of the softmax
- * sums; -infinity for a query without keys) and, where n_k > NYSTRA_DIFF_SHORT_KEYS, maps
+ * For training, sums (fp32 [n_windows][2 heads][n_q][2], 8-byte aligned: per row and map a
+ * base b and the sum of 2^(s log2 e - b) over the visible scores s; 0 for a query without
+ * keys) and, where n_k > NYSTRA_DIFF_SHORT_KEYS, maps
  * (fp32, 16-byte aligned: [n_windows][heads][n_q][d_v], the second map's output, for fp32;
  * [n_windows][heads][n_q][2][d_v], the second and the first map's, for bf16, whose O is
  * rounded) are stored for the backward pass; both are contiguous, and NULL for inference.
  * maps is NULL for shorter n_k.
  *
  * Backward: dQ, dK, dV in `dtype` (dK, dV summed over the heads that share them, zero at or
- * behind the length) and dlambda (fp32 [heads]) from dO and the same inputs, O, maps and lse.
+ * behind the length) and dlambda (fp32 [heads]) from dO and the same inputs, O, maps and sums.
  *
  * Limits: n_windows >= 0 (0: forward is a no-op, backward writes zeros to dlambda),
  * 1 <= kv_heads <= heads, 1 <= n_q, n_k <= 2^20, 1 <= d_qk <= 64, 1 <= d_v <= 128, scale
@@ -423,12 +424,12 @@ int nystra_diff_attn_workspace_size(const nystra_diff_shape *shape, int backward
 
 int nystra_diff_attn_forward(const nystra_view *Q, const nystra_view *K, const nystra_view *V,
                              const float *lambda, const int32_t *kv_len, const nystra_view *O,
-                             float *maps, float *lse, const nystra_diff_shape *shape, int dtype,
+                             float *maps, float *sums, const nystra_diff_shape *shape, int dtype,
                              void *workspace, size_t workspace_bytes, void *stream);
 
 int nystra_diff_attn_backward(const nystra_view *dO, const nystra_view *Q, const nystra_view *K,
                               const nystra_view *V, const float *lambda, const int32_t *kv_len,
-                              const nystra_view *O, const float *maps, const float *lse,
+                              const nystra_view *O, const float *maps, const float *sums,
                               const nystra_view *dQ, const nystra_view *dK, const nystra_view *dV,
                               float *dlambda, const nystra_diff_shape *shape, int dtype,
                               void *workspace, size_t workspace_bytes, void *stream);

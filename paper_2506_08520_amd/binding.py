@@ -636,19 +636,19 @@ def nystra_diff_attn_forward(q, k, v, lam, scale=0.0, causal=CAUSAL_NONE, kv_len
         _same(q, (out,))
         if out.shape != (W, H, nq, dv):
             raise ValueError(f"out must be {[W, H, nq, dv]}")
-    maps = lse = None
+    maps = sums = None
     if with_saved:
-        lse = torch.empty((W, 2 * H, nq), dtype=torch.float32, device=q.device)
+        sums = torch.empty((W, 2 * H, nq, 2), dtype=torch.float32, device=q.device)
         if nk > DIFF_SHORT_KEYS:
             # the second map's output, and in bf16, whose output is rounded, the first's
             maps = torch.empty((W, H, nq) + ((2, dv) if code == BF16 else (dv,)),
                                dtype=torch.float32, device=q.device)
     workspace, ws, nbytes = _diff_buffer(q, workspace, shape, False, code)
     rc = lib().nystra_diff_attn_forward(_view(q), _view(k), _view(v), lam.data_ptr(),
-                                        _addr(kv_len), _view(out), _addr(maps), _addr(lse),
+                                        _addr(kv_len), _view(out), _addr(maps), _addr(sums),
                                         DiffShape(*shape), code, ws, nbytes, _raw_stream(q))
     _check(rc, "nystra_diff_attn_forward")
-    return (out, (maps, lse)) if with_saved else out
+    return (out, (maps, sums)) if with_saved else out
 
 
 @_placed
@@ -660,13 +660,13 @@ def nystra_diff_attn_backward(do, q, k, v, lam, o, saved, scale=0.0, causal=CAUS
     shape = _diff_shape(q, k, v, lam, kv_len, scale, causal)
     code = _dtype_code(q)
     W, H, _, nq, nk, _, dv = shape[:7]
-    maps, lse = saved
+    maps, sums = saved
     if do.shape != (W, H, nq, dv) or o.shape != (W, H, nq, dv):
         raise ValueError(f"do and o must be {[W, H, nq, dv]}")
     _same(do, (q, o))
-    _same(do, (lse, maps), torch.float32)
+    _same(do, (sums, maps), torch.float32)
     _vector(maps, o.numel() * (2 if code == BF16 else 1), "the saved maps")
-    _vector(lse, 2 * W * H * nq, "the saved sums")
+    _vector(sums, 4 * W * H * nq, "the saved sums")
     if grads is None:
         grads = tuple(t.new_empty(t.shape) for t in (q, k, v))
     else:
@@ -677,7 +677,7 @@ def nystra_diff_attn_backward(do, q, k, v, lam, o, saved, scale=0.0, causal=CAUS
     dlam = torch.empty_like(lam)
     workspace, ws, nbytes = _diff_buffer(q, workspace, shape, True, code)
     rc = lib().nystra_diff_attn_backward(_view(do), _view(q), _view(k), _view(v), lam.data_ptr(),
-                                         _addr(kv_len), _view(o), _addr(maps), _addr(lse),
+                                         _addr(kv_len), _view(o), _addr(maps), _addr(sums),
                                          _view(dq), _view(dk), _view(dv_), dlam.data_ptr(),
                                          DiffShape(*shape), code, ws, nbytes, _raw_stream(q))
     _check(rc, "nystra_diff_attn_backward")

@@ -1087,7 +1087,7 @@ int nystra_diff_attn_workspace_size(const nystra_diff_shape *shape, int backward
 
 int nystra_diff_attn_forward(const nystra_view *Q, const nystra_view *K, const nystra_view *V,
                              const float *lambda, const int32_t *kv_len, const nystra_view *O,
-                             float *maps, float *lse, const nystra_diff_shape *shape, int dtype,
+                             float *maps, float *sums, const nystra_diff_shape *shape, int dtype,
                              void *workspace, size_t workspace_bytes, void *stream)
 {
     nystra::DiffProblem p;
@@ -1097,7 +1097,7 @@ int nystra_diff_attn_forward(const nystra_view *Q, const nystra_view *K, const n
     if (p.W == 0)
         return NYSTRA_OK;
     const int eb = dtype_bytes(dtype);
-    Range t[8] = {};   // O, maps, lse, then the inputs
+    Range t[8] = {};   // O, maps, sums, then the inputs
     if ((rc = check_view(O, p.W, p.H, p.nq, p.dv, eb, true, &p.o, &t[0])) != NYSTRA_OK ||
         (rc = check_view(Q, p.W, 2 * p.H, p.nq, p.d, eb, false, &p.q, &t[3])) != NYSTRA_OK ||
         (rc = check_view(K, p.W, 2 * p.G, p.nk, p.d, eb, false, &p.k, &t[4])) != NYSTRA_OK ||
@@ -1105,15 +1105,15 @@ int nystra_diff_attn_forward(const nystra_view *Q, const nystra_view *K, const n
         return rc;
     if (!lambda)
         return NYSTRA_ERR_NULL;
-    if (misaligned(maps, 16) || misaligned(lse, 4) || misaligned(lambda, 4) ||
+    if (misaligned(maps, 16) || misaligned(sums, 8) || misaligned(lambda, 4) ||
         misaligned(kv_len, 4))
         return NYSTRA_ERR_ALIGN;
     // The backward pass reads the maps for many keys and forms their sums itself for few.
-    if ((maps && !lse) || (lse && (maps != nullptr) != (p.nk > NYSTRA_DIFF_SHORT_KEYS)))
+    if ((maps && !sums) || (sums && (maps != nullptr) != (p.nk > NYSTRA_DIFF_SHORT_KEYS)))
         return NYSTRA_ERR_NULL;
     const int64_t rows = int64_t(p.W) * p.H * p.nq;
     t[1] = Range{maps, rows * p.dv * (eb == 2 ? 8 : 4)};
-    t[2] = Range{lse, rows * 8};
+    t[2] = Range{sums, rows * 16};
     t[6] = Range{lambda, int64_t(p.H) * 4};
     t[7] = Range{kv_len, int64_t(p.W) * 4};
     for (int i = 0; i < 3; ++i)
@@ -1124,7 +1124,7 @@ int nystra_diff_attn_forward(const nystra_view *Q, const nystra_view *K, const n
     if (rc != NYSTRA_OK)
         return rc;
     p.maps = maps;
-    p.lse = lse;
+    p.sums = sums;
     p.lambda = lambda;
     p.kv_len = kv_len;
     clear_stale_error();
@@ -1134,7 +1134,7 @@ int nystra_diff_attn_forward(const nystra_view *Q, const nystra_view *K, const n
 
 int nystra_diff_attn_backward(const nystra_view *dO, const nystra_view *Q, const nystra_view *K,
                               const nystra_view *V, const float *lambda, const int32_t *kv_len,
-                              const nystra_view *O, const float *maps, const float *lse,
+                              const nystra_view *O, const float *maps, const float *sums,
                               const nystra_view *dQ, const nystra_view *dK, const nystra_view *dV,
                               float *dlambda, const nystra_diff_shape *shape, int dtype,
                               void *workspace, size_t workspace_bytes, void *stream)
@@ -1160,14 +1160,14 @@ int nystra_diff_attn_backward(const nystra_view *dO, const nystra_view *Q, const
             (rc = check_view(V, p.W, p.G, p.nk, p.dv, eb, false, &p.v, &t[7])) != NYSTRA_OK ||
             (rc = check_view(O, p.W, p.H, p.nq, p.dv, eb, false, &p.o, &t[8])) != NYSTRA_OK)
             return rc;
-        if (!lambda || !lse || (maps != nullptr) != (p.nk > NYSTRA_DIFF_SHORT_KEYS))
+        if (!lambda || !sums || (maps != nullptr) != (p.nk > NYSTRA_DIFF_SHORT_KEYS))
             return NYSTRA_ERR_NULL;
-        if (misaligned(maps, 16) || misaligned(lse, 4) || misaligned(lambda, 4) ||
+        if (misaligned(maps, 16) || misaligned(sums, 8) || misaligned(lambda, 4) ||
             misaligned(kv_len, 4))
             return NYSTRA_ERR_ALIGN;
         t[3] = Range{dlambda, int64_t(p.H) * 4};
         t[9] = Range{maps, rows * p.dv * (eb == 2 ? 8 : 4)};
-        t[10] = Range{lse, rows * 8};
+        t[10] = Range{sums, rows * 16};
         t[11] = Range{lambda, int64_t(p.H) * 4};
         t[12] = Range{kv_len, int64_t(p.W) * 4};
         for (int i = 0; i < 4; ++i)
@@ -1181,7 +1181,7 @@ int nystra_diff_attn_backward(const nystra_view *dO, const nystra_view *Q, const
     }
     p.maps = const_cast<float *>(maps);
     p.glam = dlambda;
-    p.lse = const_cast<float *>(lse);
+    p.sums = const_cast<float *>(sums);
     p.lambda = lambda;
     p.kv_len = kv_len;
     clear_stale_error();

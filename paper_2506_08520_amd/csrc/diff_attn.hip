@@ -144,10 +144,10 @@ diff_forward_kernel(DiffProblem p)
                     store4<F32>(maps + p.dv, col, p.dv, p.dv % 4 == 0, x[0], x[1], x[2], x[3]);
             }
         }
-    if (p.lse && g == 0) {
-        float *lse = p.lse + (int64_t(w) * 2 * p.H + 2 * row.head) * p.nq + row.token;
-        lse[0] = l[0] == 0.f ? -INFINITY : m[0] + log2f(l[0]);
-        lse[p.nq] = l[1] == 0.f ? -INFINITY : m[1] + log2f(l[1]);
+    if (p.sums && g == 0) {
+        float2 *sums = sum_row(p, w, row);
+        sums[0] = make_float2(m[0], l[0]);
+        sums[p.nq] = make_float2(m[1], l[1]);
     }
 }
 
@@ -201,11 +201,10 @@ diff_merge_few_kernel(DiffProblem p, int64_t items)
         if (E::bytes == 2)
             store4<F32>(maps + p.dv, col, p.dv, p.dv % 4 == 0, x[0][0], x[0][1], x[0][2], x[0][3]);
     }
-    if (p.lse && col == 0) {
-        float *lse = p.lse + (int64_t(w) * 2 * p.H + 2 * row.head) * p.nq + row.token;
+    if (p.sums && col == 0) {
 #pragma unroll
         for (int a = 0; a < 2; ++a)
-            lse[a * p.nq] = l[a] == 0.f ? -INFINITY : m[a] + log2f(l[a]);
+            sum_row(p, w, row)[a * p.nq] = make_float2(m[a], l[a]);
     }
 }
 
@@ -257,9 +256,8 @@ diff_merge_kernel(DiffProblem p)
             }
         }
         out[a][i - a * p.dv4] = l == 0.f ? 0.f : x / l;
-        if (p.lse && i == a * p.dv4)
-            p.lse[(int64_t(w) * 2 * p.H + 2 * row.head + a) * p.nq + row.token] =
-                l == 0.f ? -INFINITY : m + log2f(l);
+        if (p.sums && i == a * p.dv4)
+            sum_row(p, w, row)[a * p.nq] = make_float2(m, l);
     }
     __syncthreads();
     const float lam = p.lambda[row.head];

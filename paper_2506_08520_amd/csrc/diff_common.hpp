@@ -455,6 +455,14 @@ __device__ inline void store4(typename E::T *row, int col, int n, bool vec, floa
         }
 }
 
+// The exponents' base and the sum of a row's exponentials for its first map, in
+// [W][2 H][n_q][2]; the second map's lie n_q behind.
+__device__ inline float2 *sum_row(const DiffProblem &p, int w, const Row &row)
+{
+    return reinterpret_cast<float2 *>(p.sums) +
+           (int64_t(w) * 2 * p.H + 2 * row.head) * p.nq + row.token;
+}
+
 // What is kept of a row for the backward pass, in fp32: the second map's output, and
 // where O itself is rounded to bf16 the first one's, in [W][H][n_q][1 or 2][d_v].
 template <class E>

@@ -19,7 +19,9 @@ __device__ inline float dot8(const Frag<E> &a, const Chunk<F32> &b)
     return s;
 }
 
-// dQ, and per row D_1, D_2 and -dlam.  Rows as in the forward pass.  D_a comes from the
+// dQ, and per row D_1, D_2 and -dlam.  Rows as in the forward pass.  The exponentials are
+// the forward pass's, bit by bit, and their sums divide what is formed from them, so that
+// every row's probabilities add up to one and dlam, a sum of both signs, keeps its digits.  D_a comes from the
 // maps' outputs, D_2 = dO . O_2 and D_1 = dO . O_1 (fp32: dO . O + lam D_2), which the
 // forward pass keeps in fp32 (from outputs rounded to bf16, dQ was off by 0.0030 of its norm
 // at 4096 keys where rounding it alone costs 0.0017), or, where it kept none (few keys), from
@@ -53,7 +55,7 @@ diff_dq_kernel(DiffProblem p)
     if (kend > 0)
         tiles.fetch(p, k0, v0, 0, kend, buf);
     Frag<E> q[2][DK / 16], go[DV / 16];
-    float L[2], D[2] = {0.f, 0.f};
+    float base[2], inv[2], D[2] = {0.f, 0.f};
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
         const T *src = at<E>(p.q, w, 2 * row.head + a, row.token);
@@ -61,8 +63,9 @@ diff_dq_kernel(DiffProblem p)
         for (int i = 0; i < DK / 16; ++i)
             q[a][i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
                                                        p.d - 16 * i - 8 * g, live, p.d));
-        L[a] = limit > 0 ? p.lse[(int64_t(w) * 2 * p.H + 2 * row.head + a) * p.nq + row.token]
-                         : INFINITY;   // exp2(-inf) = 0 where no key is seen
+        const float2 sum = sum_row(p, w, row)[a * p.nq];
+        base[a] = limit > 0 ? sum.x : INFINITY;   // exp2(-inf) = 0 where no key is seen
+        inv[a] = limit > 0 && sum.y != 0.f ? 1.f / sum.y : 0.f;
     }
     const T *gosrc = at<E>(p.go, w, row.head, row.token);
 #pragma unroll
@@ -85,6 +88,7 @@ diff_dq_kernel(DiffProblem p)
         for (int a = 0; a < 2; ++a)
             D[a] = half_sum(D[a]);
     }
+    const float w1 = inv[0], w2 = -lam * inv[1];
     f16v acc[2][DK / 32] = {};
     float glam = 0.f;
     if (kend > 0)
@@ -120,7 +124,7 @@ diff_dq_kernel(DiffProblem p)
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        s[a][i] = fast_exp2(fmaf(s[a][i], p.scale2, -L[a]));
+                        s[a][i] = fast_exp2(fmaf(s[a][i], p.scale2, -base[a]));
                 if (sweep == 0) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
@@ -130,9 +134,10 @@ diff_dq_kernel(DiffProblem p)
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
+                        // the sums of the exponentials divide the other factor
                         glam = fmaf(s[1][i], x[i], glam);
-                        s[0][i] *= x[i] - D[0];
-                        s[1][i] *= fmaf(-lam, x[i], lam * D[1]);
+                        s[0][i] *= fmaf(w1, x[i], -w1 * D[0]);
+                        s[1][i] *= fmaf(w2, x[i], -w2 * D[1]);
                     }
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
@@ -152,15 +157,16 @@ diff_dq_kernel(DiffProblem p)
         if (sweep == 0) {
 #pragma unroll
             for (int a = 0; a < 2; ++a)
-                D[a] = half_sum(sum[a]);
+                D[a] = half_sum(sum[a]) * inv[a];
         }
     }
-    glam = half_sum(glam);
+    glam = half_sum(glam) * inv[1];
     // What the dK, dV kernel needs of a row, also for those up to the end of the last tile
     // of 32.
     if (g == 0 && r < p.rows32) {
-        p.row_stats[unit * p.rows32 + r] = limit > 0 ? make_float4(L[0], L[1], D[0], D[1])
-                                                     : make_float4(L[0], L[1], 0.f, 0.f);
+        p.row_stats[unit * p.rows32 + r] =
+            limit > 0 ? make_float4(base[0] - log2f(inv[0]), base[1] - log2f(inv[1]), D[0], D[1])
+                      : make_float4(INFINITY, INFINITY, 0.f, 0.f);
         p.row_lambda[unit * p.rows32 + r] = lam;
     }
     if (!live)

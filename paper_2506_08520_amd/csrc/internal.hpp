@@ -135,7 +135,7 @@ struct DiffView {
 struct DiffProblem {
     DiffView q, k, v, o, go, gq, gk, gv;   // Q and K hold two heads per query / key head
     float *maps;           // [W][H][nq][1 or 2][dv], the maps' outputs, or null
-    float *lse;            // [W][2H][nq], log2 of the sums of exponentials, or null
+    float *sums;           // [W][2H][nq][2]: exponents' base, sum of exponentials, or null
     const float *lambda;   // [H]
     const int32_t *kv_len; // [W] or null
     int W, H, G, R;        // windows, query heads, key heads, H / G

@@ -79,8 +79,8 @@ class _DiffAttention(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, do):
         _not_recorded_backward()
-        q, k, v, lam, o, kv_len, maps, lse = ctx.saved_tensors
-        grads = B.nystra_diff_attn_backward(do.contiguous(), q, k, v, lam, o, (maps, lse),
+        q, k, v, lam, o, kv_len, maps, sums = ctx.saved_tensors
+        grads = B.nystra_diff_attn_backward(do.contiguous(), q, k, v, lam, o, (maps, sums),
                                             kv_len=kv_len, **ctx.args)
         return (*grads, None, None, None)
 
@@ -110,12 +110,12 @@ class _PackedDiffAttention(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, do):
         _not_recorded_backward()
-        qkv, lam, out, maps, lse = ctx.saved_tensors
+        qkv, lam, out, maps, sums = ctx.saved_tensors
         heads = out.shape[2]
         grad = torch.empty_like(qkv)
         *_, dlam = B.nystra_diff_attn_backward(
             do.contiguous().transpose(1, 2), *_packed_views(qkv, heads), lam,
-            out.transpose(1, 2), (maps, lse), grads=_packed_views(grad, heads))
+            out.transpose(1, 2), (maps, sums), grads=_packed_views(grad, heads))
         return grad, dlam, None
 
 

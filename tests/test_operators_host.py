@@ -99,18 +99,18 @@ def views(s):
                 dk=c(A[6], 2 * G, nk, d), dv=c(A[7], G, nk, dv))
 
 
-def forward(L, s=None, lam=A[8], kv=None, maps=A[9], lse=A[10], dtype=1, ws=None, wsb=0, **kw):
+def forward(L, s=None, lam=A[8], kv=None, maps=A[9], sums=A[10], dtype=1, ws=None, wsb=0, **kw):
     s = shape() if s is None else s
     t = {**views(s), **kw}
-    return L.nystra_diff_attn_forward(t["q"], t["k"], t["v"], lam, kv, t["o"], maps, lse, s, dtype,
+    return L.nystra_diff_attn_forward(t["q"], t["k"], t["v"], lam, kv, t["o"], maps, sums, s, dtype,
                                       ws, wsb, None)
 
 
-def backward(L, s=None, lam=A[8], kv=None, maps=A[9], lse=A[10], dlam=A[11], dtype=1, ws=A[12],
+def backward(L, s=None, lam=A[8], kv=None, maps=A[9], sums=A[10], dlam=A[11], dtype=1, ws=A[12],
              wsb=1 << 23, **kw):
     s = shape() if s is None else s
     t = {**views(s), **kw}
-    return L.nystra_diff_attn_backward(t["do"], t["q"], t["k"], t["v"], lam, kv, t["o"], maps, lse,
+    return L.nystra_diff_attn_backward(t["do"], t["q"], t["k"], t["v"], lam, kv, t["o"], maps, sums,
                                        t["dq"], t["dk"], t["dv"], dlam, s, dtype, ws, wsb, None)
 
 
@@ -150,18 +150,18 @@ def test_diff_attention_tensors(L, call, outputs):
         assert call(L, **{name: B.View(A[8], v.window, v.head, v.token)}) == EOVERLAP, name
     assert call(L, lam=None) == ENULL
     assert call(L, lam=A[8] + 2) == EALIGN and call(L, kv=A[13] + 2) == EALIGN
-    assert call(L, lse=A[10] + 2) == EALIGN
+    assert call(L, sums=A[10] + 2) == EALIGN
 
 
 def test_diff_attention_saved_values(L):
     # many keys: both; few: the sums alone; inference: neither
-    assert forward(L, lse=None) == ENULL
+    assert forward(L, sums=None) == ENULL
     assert forward(L, maps=None) == ENULL
     assert forward(L, s=shape(nk=128)) == ENULL
-    assert backward(L, maps=None) == ENULL and backward(L, lse=None) == ENULL
+    assert backward(L, maps=None) == ENULL and backward(L, sums=None) == ENULL
     assert backward(L, s=shape(nk=128)) == ENULL
     assert backward(L, dlam=None) == ENULL and backward(L, dlam=A[11] + 1) == EALIGN
-    assert forward(L, lse=A[3]) == EOVERLAP and forward(L, maps=A[0]) == EOVERLAP
+    assert forward(L, sums=A[3]) == EOVERLAP and forward(L, maps=A[0]) == EOVERLAP
     assert backward(L, dlam=A[5]) == EOVERLAP and backward(L, dlam=A[8]) == EOVERLAP
 
 
@@ -175,14 +175,14 @@ def test_diff_attention_workspaces(L):
     assert need > 0
     for kw in [dict(ws=None, wsb=need), dict(ws=A[12], wsb=need - 1), dict(ws=A[12] + 4, wsb=need),
                dict(ws=A[3], wsb=need)]:
-        assert forward(L, s=s, maps=None, lse=None, **kw) == EWS, kw
+        assert forward(L, s=s, maps=None, sums=None, **kw) == EWS, kw
     assert B.nystra_diff_attn_workspace_size(shape(W=0), True) == 0
 
 
 def test_no_windows_is_a_no_op(L):
     null = B.View(None, 0, 0, 0)
     s = shape(W=0)
-    assert forward(L, s=s, q=null, k=null, v=null, o=null, lam=None, maps=None, lse=None) == OK
+    assert forward(L, s=s, q=null, k=null, v=null, o=null, lam=None, maps=None, sums=None) == OK
 
 
 def test_binding_refuses_host_tensors():
