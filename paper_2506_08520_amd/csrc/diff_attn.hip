@@ -12,7 +12,7 @@ constexpr int kMerge = 256;       // threads of the merge kernel: one row
 constexpr int kFewSplits = 8;
 
 template <class E, int DK, int DV, int NW, bool DIRECT>
-__global__ void __launch_bounds__(64 * NW, (NW == 1 && !DIRECT ? 1 : occupancy<E, DV>()))
+__global__ void __launch_bounds__(64 * NW, (NW == 1 && !DIRECT ? 1 : occupancy<E, DV>(NW == 2 && DV == 64)))
 diff_forward_kernel(DiffProblem p)
 {
     using T = typename E::T;
@@ -21,11 +21,9 @@ diff_forward_kernel(DiffProblem p)
     __shared__ alignas(256) char lds[2 * Tiles::kBuffer];
     const uint32_t buf = lds_offset(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
-    int64_t b = xcd_order(blockIdx.x, gridDim.x);
-    const int split = int(b % p.splits);
-    b /= p.splits;
-    const int tile = int(b % p.tiles);
-    const int64_t unit = b / p.tiles;
+    const Place here = place(p, blockIdx.x, gridDim.x, p.tiles, p.splits, true);
+    const int64_t unit = here.unit;
+    const int tile = here.tile, split = here.split;
     const int w = int(unit / p.G), kvh = int(unit % p.G);
     const int nrows = p.R * p.nq;
     const int r0 = tile * 32 * NW, r = r0 + wave * 32 + c;
@@ -47,7 +45,7 @@ diff_forward_kernel(DiffProblem p)
         const T *src = at<E>(p.q, w, 2 * row.head + a, row.token);
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
-            q[a][i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
+            q[a][i] = as_frag(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
                                                        p.d - 16 * i - 8 * g, live, p.d));
     }
     f16v acc[2][DV / 32] = {};
@@ -68,7 +66,7 @@ diff_forward_kernel(DiffProblem p)
             for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
                 for (int a = 0; a < 2; ++a)
-                    s[a] = mma(row_frag<E>(krow + a * KT * Tiles::LK::pitch, i), q[a][i], s[a]);
+                    s[a] = mma(row_frag<E, DK>(krow + a * Tiles::LK::kBytes, i), q[a][i], s[a]);
             part();
             if (!__all(key + KT <= limit)) {
                 hide(s[0], limit, key, g);
@@ -281,9 +279,8 @@ struct Plan {
 };
 
 // Key ranges: with few rows enough of them for eight waves on each of the 256 CUs, of at
-// least one tile to a wave.  Workgroups of more waves are split only below one to a CU: 5 x 25
-// of them over 777 keys (fp32, causal) took 196 us in one range and in three, and joining
-// the three another 72 us.
+// least one tile to a wave.  Workgroups of more waves are split only below one to a CU, or
+// three under a causal mask, where the longest ones would be waited for.
 Plan forward_plan(const DiffProblem &p)
 {
     Plan f;
@@ -292,7 +289,8 @@ Plan forward_plan(const DiffProblem &p)
     f.tiles = ceil_div(rows, 32 * f.waves);
     const int64_t blocks = int64_t(p.W) * p.G * f.tiles;
     const int64_t want = std::max<int64_t>(f.waves == 1 ? (2048 + blocks - 1) / blocks
-                                                        : 1024 / f.waves / blocks, 1);
+                                                        : (p.causal == 0 ? 1024 : 3072) / f.waves / blocks,
+                                               1);
     const int64_t most = ceil_div(p.nk, 32 * f.waves);
     f.splits = int(std::min(want, most));
     f.chunk = ceil_div(ceil_div(p.nk, f.splits), 32) * 32;

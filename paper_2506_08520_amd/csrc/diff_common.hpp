@@ -21,7 +21,9 @@
 // register r.  Which index a slot stands for is free as long as both operands
 // agree: operands read along rows (row_frag) use 8 g + j, those that meet a
 // product's result (col_frag) use that result's order, 8 (j / 4) + 4 g + j % 4.
-// bf16 runs it as one matrix instruction, fp32 as eight of depth two.
+// bf16 runs it as one matrix instruction.  fp32 operands are carried as three bf16 terms
+// (24 bits), whose six largest products make a product: 192 cycles against 512 of the eight
+// fp32 instructions of depth two, and within 2^-22 of it.
 #pragma once
 
 #include "device_common.hpp"
@@ -44,9 +46,11 @@ struct Frag<BF16> {
     bf8 x;
 };
 
+// x = h + m + l: h is x cut off at bf16, m and l are rounded to nearest even; exact down to
+// |x| = 2^-110.  An infinity becomes NaN (its rest is inf - inf).
 template <>
 struct Frag<F32> {
-    float x[8];
+    bf8 h, m, l;
 };
 
 __device__ inline f16v mma(const Frag<BF16> &a, const Frag<BF16> &b, f16v c)
@@ -54,12 +58,35 @@ __device__ inline f16v mma(const Frag<BF16> &a, const Frag<BF16> &b, f16v c)
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x, b.x, c, 0, 0, 0);
 }
 
+// The small products first; those left out (m l, l m, l l) are below 2^-22 of the whole.
 __device__ inline f16v mma(const Frag<F32> &a, const Frag<F32> &b, f16v c)
 {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.l, b.h, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.h, b.l, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.m, b.m, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.m, b.h, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.h, b.m, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.h, b.h, c, 0, 0, 0);
+}
+
+__device__ inline Frag<F32> split(const float (&x)[8])
+{
+    typedef float f8 __attribute__((ext_vector_type(8)));
+    typedef uint32_t h8 __attribute__((ext_vector_type(4)));
+    Frag<F32> f;
+    h8 h;
+    f8 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)   // the upper halves of two
+        h[j] = __builtin_amdgcn_perm(__float_as_uint(x[2 * j + 1]), __float_as_uint(x[2 * j]),
+                                     0x07060302u);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[j], b.x[j], c, 0, 0, 0);
-    return c;
+        r[j] = x[j] - __uint_as_float(__float_as_uint(x[j]) & 0xffff0000u);
+    f.h = __builtin_bit_cast(bf8, h);
+    f.m = __builtin_convertvector(r, bf8);
+    f.l = __builtin_convertvector(r - __builtin_convertvector(f.m, f8), bf8);
+    return f;
 }
 
 // Eight consecutive elements as they lie in memory.
@@ -130,10 +157,18 @@ __device__ inline Chunk<E> load_chunk(const typename E::T *p, int n, bool live, 
     return c;
 }
 
-template <class E>
-__device__ inline Frag<E> as_frag(const Chunk<E> &c)
+__device__ inline Frag<BF16> as_frag(const Chunk<BF16> &c)
 {
-    return __builtin_bit_cast(Frag<E>, c);
+    return __builtin_bit_cast(Frag<BF16>, c);
+}
+
+__device__ inline Frag<F32> as_frag(const Chunk<F32> &c)
+{
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        x[j] = __uint_as_float(c.w[j]);
+    return split(x);
 }
 
 __device__ inline Frag<BF16> frag_of(const f16v &s, int c, BF16)
@@ -148,11 +183,11 @@ __device__ inline Frag<BF16> frag_of(const f16v &s, int c, BF16)
 
 __device__ inline Frag<F32> frag_of(const f16v &s, int c, F32)
 {
-    Frag<F32> f;
+    float x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        f.x[j] = s[8 * c + j];
-    return f;
+        x[j] = s[8 * c + j];
+    return split(x);
 }
 
 // LDS is addressed by byte offsets.
@@ -167,29 +202,6 @@ __device__ inline __attribute__((address_space(3))) T *lds_at(uint32_t at)
     return (__attribute__((address_space(3))) T *)(uintptr_t(at));
 }
 
-template <class E>
-__device__ inline Chunk<E> lds_chunk(uint32_t at)
-{
-    Chunk<E> c;
-#pragma unroll
-    for (int h = 0; h < E::bytes / 2; ++h) {
-        const u4 x = *lds_at<u4>(at + 16 * h);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            c.w[4 * h + j] = x[j];
-    }
-    return c;
-}
-
-template <class E>
-__device__ inline void set_lds_chunk(uint32_t at, const Chunk<E> &c)
-{
-#pragma unroll
-    for (int h = 0; h < E::bytes / 2; ++h)
-        *lds_at<u4>(at + 16 * h) =
-            (u4){c.w[4 * h], c.w[4 * h + 1], c.w[4 * h + 2], c.w[4 * h + 3]};
-}
-
 __device__ inline void exchange(uint32_t &a, uint32_t &b)
 {
     const uint32_t x = a;
@@ -197,28 +209,39 @@ __device__ inline void exchange(uint32_t &a, uint32_t &b)
     b = x;
 }
 
-// A tile of rows of COLS elements in LDS, in chunks of eight elements.  Row fragments read
-// the same chunk of eight rows at a time, the transposing reads below two neighbouring
-// chunks of four rows; over the 64 banks of 4 bytes neither may meet a bank twice.  bf16
-// rows lie without gaps (so that loads can go to LDS directly) with their chunks exchanged
-// by a number from the row; fp32 rows, which have no transposing reads, are 16 bytes apart.
-// A bf16 tile starts at a multiple of 256 bytes, so that the fragments of a tile follow
-// from the first one's address by an exclusive or (one instruction and no register each).
+// A tile of 32 rows of COLS elements in LDS, in chunks of eight elements, fp32 as one plane
+// for each of its three terms.  Row fragments read the same chunk of eight rows at a time, the
+// transposing reads below two neighbouring chunks of four rows; over the 64 banks of 4 bytes
+// neither may meet a bank twice.  Rows lie without gaps (so that loads can go to LDS directly)
+// with their chunks exchanged by a number from the row.  A tile starts at a multiple of 256
+// bytes, so that its fragments follow from the first one's address by an exclusive or (one
+// instruction and no register each).
 template <class E, int COLS>
 struct Tile {
-    static constexpr int pitch = E::bytes == 2 ? 2 * COLS : 4 * COLS + 16;   // bytes
+    static constexpr int pitch = 2 * COLS;   // bytes
     static constexpr int kRow = COLS / 8;
+    static constexpr uint32_t kPlane = 32 * pitch;
+    static constexpr uint32_t kBytes = E::bytes == 2 ? kPlane : 3 * kPlane;
 
     __device__ static inline int swap(int row)
     {
-        if constexpr (E::bytes == 4)
-            return 0;
-        else
-            return COLS == 32 ? (row >> 2) & 3 : COLS == 64 ? row & 7 : (row & 7) << 1;
+        return COLS == 32 ? (row >> 2) & 3 : COLS == 64 ? row & 7 : (row & 7) << 1;
     }
     __device__ static inline uint32_t at(int row, int chunk)
     {
-        return row * pitch + 8 * E::bytes * (chunk ^ swap(row));
+        return row * pitch + 16 * (chunk ^ swap(row));
+    }
+    __device__ static inline void store(uint32_t tile, int row, int chunk, const Chunk<E> &c)
+    {
+        const Frag<E> f = as_frag(c);
+        const uint32_t to = tile + at(row, chunk);
+        if constexpr (E::bytes == 2) {
+            *lds_at<bf8>(to) = f.x;
+        } else {
+            *lds_at<bf8>(to) = f.h;
+            *lds_at<bf8>(to + kPlane) = f.m;
+            *lds_at<bf8>(to + 2 * kPlane) = f.l;
+        }
     }
 };
 
@@ -231,56 +254,57 @@ __device__ inline uint32_t first_row(uint32_t tile)
     return tile + Tile<E, COLS>::at(lane & 31, lane >> 5);
 }
 
-template <class E>
+template <class E, int COLS>
 __device__ inline Frag<E> row_frag(uint32_t first, int c)
 {
-    if constexpr (E::bytes == 2) {
-        return as_frag<E>(lds_chunk<E>(first ^ (32 * c)));
-    } else {
-        return as_frag<E>(lds_chunk<E>(first + 64 * c));
-    }
+    constexpr uint32_t plane = Tile<E, COLS>::kPlane;
+    const uint32_t at = first ^ (32 * c);
+    if constexpr (E::bytes == 2)
+        return Frag<E>{*lds_at<bf8>(at)};
+    else
+        return Frag<E>{*lds_at<bf8>(at), *lds_at<bf8>(at + plane), *lds_at<bf8>(at + 2 * plane)};
 }
 
 // Column fragments: column 32 i + lane % 32, contraction indices (rows) in the order of a
-// product's result, 16 c + 8 (j / 4) + 4 g + j % 4.  In bf16 the transposing LDS read
-// takes four rows of 16 columns from 16 lanes (lane p: row p / 4, columns 4 (p % 4) ..) and
-// gives each lane its column of them.
+// product's result, 16 c + 8 (j / 4) + 4 g + j % 4.  The transposing LDS read takes four rows
+// of 16 columns from 16 lanes (lane p: row p / 4, columns 4 (p % 4) ..) and gives each lane
+// its column of them.
 template <class E, int COLS>
 __device__ inline uint32_t first_col(uint32_t tile)
 {
-    const int lane = threadIdx.x & 63, g = lane >> 5;
-    if constexpr (E::bytes == 2) {
-        const int col = (lane & 16) + 4 * (lane & 3);
-        return tile + Tile<E, COLS>::at(4 * g + ((lane & 15) >> 2), col >> 3) + 2 * (col & 7);
-    } else {
-        return tile + 4 * g * Tile<E, COLS>::pitch + 4 * (lane & 31);
-    }
+    const int lane = threadIdx.x & 63;
+    const int col = (lane & 16) + 4 * (lane & 3);
+    return tile + Tile<E, COLS>::at(4 * (lane >> 5) + ((lane & 15) >> 2), col >> 3) +
+           2 * (col & 7);
+}
+
+template <int COLS>
+__device__ inline bf8 col_plane(uint32_t first, int c, int i)
+{
+    constexpr int pitch = 2 * COLS;
+    const uint32_t lo = (first ^ (64 * i)) + 16 * c * pitch;
+    // Eight rows on, rows of four chunks have theirs exchanged by another number.
+    const uint32_t hi = (COLS == 32 ? first ^ 32 : first ^ (64 * i)) + (16 * c + 8) * pitch;
+    struct {
+        s4 lo, hi;
+    } v;
+    v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s4>(lo));
+    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s4>(hi));
+    return __builtin_bit_cast(bf8, v);
 }
 
 template <class E, int COLS>
 __device__ inline Frag<E> col_frag(uint32_t first, int c, int i)
 {
-    constexpr int pitch = Tile<E, COLS>::pitch;
-    if constexpr (E::bytes == 2) {
-        const uint32_t lo = (first ^ (64 * i)) + 16 * c * pitch;
-        // Eight rows on, rows of four chunks have theirs exchanged by another number.
-        const uint32_t hi = (COLS == 32 ? first ^ 32 : first ^ (64 * i)) + (16 * c + 8) * pitch;
-        struct {
-            s4 lo, hi;
-        } v;
-        v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s4>(lo));
-        v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s4>(hi));
-        return __builtin_bit_cast(Frag<BF16>, v);
-    } else {
-        Frag<F32> f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            f.x[j] = *lds_at<float>(first + (16 * c + 8 * (j >> 2) + (j & 3)) * pitch + 128 * i);
-        return f;
-    }
+    constexpr uint32_t plane = Tile<E, COLS>::kPlane;
+    if constexpr (E::bytes == 2)
+        return Frag<E>{col_plane<COLS>(first, c, i)};
+    else
+        return Frag<E>{col_plane<COLS>(first, c, i), col_plane<COLS>(first + plane, c, i),
+                       col_plane<COLS>(first + 2 * plane, c, i)};
 }
 
-// Walks a [rows][COLS] tile in chunks of eight elements over the NT threads of a
+// Walks tiles of together ROWS rows in chunks of eight elements over the NT threads of a
 // workgroup: loaded into registers while the tile before it is worked on, stored to LDS
 // when that is done.
 template <class E, int COLS, int ROWS, int NT>
@@ -310,7 +334,7 @@ struct Stage {
         for (int i = 0; i < kN; ++i) {
             const int id = threadIdx.x + i * NT;
             if (kAll % NT == 0 || id < kAll)
-                set_lds_chunk<E>(lds + L::at(id / L::kRow, id % L::kRow), x[i]);
+                L::store(lds + id / L::kRow / 32 * L::kBytes, id / L::kRow % 32, id % L::kRow, x[i]);
         }
     }
 };
@@ -522,12 +546,36 @@ __device__ inline void softmax_step(f16v &s, float scale2, float &m, float &l, G
     l += sum;
 }
 
-// Blocks of one unit run on one XCD (blocks go to the eight of them in turn), so
-// that the unit's keys and values are fetched into one L2 only.
-__device__ inline int64_t xcd_order(int64_t b, int64_t n)
+// Which unit, tile and range a workgroup takes.  Even work: the workgroups of a unit run on
+// one XCD (workgroups go to the eight of them in turn), so that its keys and values are
+// fetched into one L2 only.  Uneven work (causal masks, lengths): the tiles with the most
+// keys of all units first, over all XCDs.
+struct Place {
+    int64_t unit;
+    int tile, split;
+};
+
+__device__ inline Place place(const DiffProblem &p, int64_t b, int64_t n, int tiles, int splits,
+                              bool last_first)
 {
-    const int64_t per = n / 8, full = per * 8;
-    return b < full ? (b % 8) * per + b / 8 : b;
+    Place at;
+    if (p.even) {
+        const int64_t per = n / 8, full = per * 8;
+        b = b < full ? (b % 8) * per + b / 8 : b;
+        at.split = int(b % splits);
+        b /= splits;
+        at.tile = int(b % tiles);
+        at.unit = b / tiles;
+    } else {
+        const int64_t units = int64_t(p.W) * p.G;
+        at.unit = b % units;
+        b /= units;
+        at.split = int(b % splits);
+        at.tile = int(b / splits);
+        if (last_first)
+            at.tile = tiles - 1 - at.tile;
+    }
+    return at;
 }
 
 // Keys and values of a unit, tile after tile of KT keys, into two LDS buffers in turn:
@@ -540,7 +588,7 @@ struct KeyTiles {
     using LK = Tile<E, DK>;
     using LV = Tile<E, DV>;
     // One buffer in LDS: the keys of both maps, then the values.
-    static constexpr uint32_t kV = 2 * KT * LK::pitch, kBuffer = kV + KT * LV::pitch;
+    static constexpr uint32_t kV = 2 * LK::kBytes, kBuffer = kV + LV::kBytes;
     Stage<E, DK, 2 * KT, NT> k;   // both maps, one under the other
     Stage<E, DV, KT, NT> v;
 
@@ -585,12 +633,13 @@ struct KeyTiles {
 __device__ inline void part() { __builtin_amdgcn_sched_barrier(0); }
 
 // Waves to a SIMD that the kernels are compiled for: two, whose matrix instructions and
-// exponentials run beside each other, except at full width for fp32 and for kernels with `more`
-// to hold, whose operands do not fit 256 registers.
+// exponentials run beside each other, or one for kernels with `more` to hold than 256
+// registers: at full width, or fp32, whose operands take three terms; at full width fp32
+// always.
 template <class E, int DV>
-constexpr int occupancy(bool more = false)
+constexpr int occupancy(bool more)
 {
-    return DV == 128 && (E::bytes == 4 || more) ? 1 : 2;
+    return DV == 128 ? (E::bytes == 4 || more ? 1 : 2) : (E::bytes == 4 && more ? 1 : 2);
 }
 
 // ---- host side ----------------------------------------------------------------
@@ -627,6 +676,8 @@ inline bool narrow(const DiffProblem &p) { return p.d <= 32 && p.dv <= 64; }
 
 inline void set_common(DiffProblem *p)
 {
+    // With many units uneven work evens out, and each still has an L2 to itself.
+    p->even = (p->causal == 0 && !p->kv_len) || int64_t(p->W) * p->G >= 512;
     p->nq_shift = 31 + (31 - __builtin_clz(unsigned(p->nq)));
     p->nq_mul = uint32_t(((uint64_t(1) << p->nq_shift) + p->nq - 1) / p->nq);
 }

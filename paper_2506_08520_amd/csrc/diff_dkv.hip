@@ -51,7 +51,7 @@ __device__ inline float key_scale(const DiffProblem &p, int len)
 // length get zeros.  With few workgroups the rows are split over p.rsplits of them, whose
 // sums go to the workspace.  The first H workgroups add up dlam meanwhile.
 template <class E, int DK, int DV, int NW, bool DIRECT>
-__global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>()))
+__global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>(E::bytes == 4)))
 diff_dkv_kernel(DiffProblem p)
 {
     using T = typename E::T;
@@ -62,21 +62,19 @@ diff_dkv_kernel(DiffProblem p)
     constexpr bool kLdsV = E::bytes == 2 && DV == 128;
     // A buffer in LDS: the queries of both maps, dO, and per row L_1, L_2, D_1, D_2, lam
     // and the keys that it sees.
-    constexpr uint32_t kMap = QT * LQ::pitch, kGo = 2 * kMap, kStat = kGo + QT * LG::pitch;
+    constexpr uint32_t kMap = LQ::kBytes, kGo = 2 * kMap, kStat = kGo + LG::kBytes;
     constexpr uint32_t kLam = kStat + 16 * QT, kLim = kLam + 4 * QT;
     constexpr uint32_t kBuffer = (kLim + 4 * QT + 255) / 256 * 256;
-    __shared__ alignas(256) char lds[2 * kBuffer + (kLdsV ? NW * 32 * LG::pitch : 0)];
+    __shared__ alignas(256) char lds[2 * kBuffer + (kLdsV ? NW * LG::kBytes : 0)];
     const uint32_t buf = lds_offset(lds), vs = buf + 2 * kBuffer;
     if (int(blockIdx.x) < p.H) {
         sum_dlam<NT>(p, blockIdx.x, p.glam);
         return;
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
-    int64_t b = xcd_order(blockIdx.x - p.H, gridDim.x - p.H);
-    const int split = int(b % p.rsplits);
-    b /= p.rsplits;
-    const int tile = int(b % p.ktiles);
-    const int64_t unit = b / p.ktiles;
+    const Place here = place(p, blockIdx.x - p.H, gridDim.x - p.H, p.ktiles, p.rsplits, false);
+    const int64_t unit = here.unit;
+    const int tile = here.tile, split = here.split;
     const int w = int(unit / p.G), kvh = int(unit % p.G);
     const int nrows = p.R * p.nq;
     const int kb = tile * 32 * NW, kw = kb + wave * 32, key = kw + c;
@@ -89,7 +87,7 @@ diff_dkv_kernel(DiffProblem p)
         const T *src = at<E>(p.k, w, 2 * kvh + a, live ? key : 0);
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
-            k[a][i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
+            k[a][i] = as_frag(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
                                                        p.d - 16 * i - 8 * g, live, p.d));
     }
     if constexpr (kLdsV) {
@@ -99,15 +97,15 @@ diff_dkv_kernel(DiffProblem p)
         for (int i = 0; i < kChunks; ++i) {
             const int id = threadIdx.x + i * NT, row = id / LG::kRow, ch = id % LG::kRow;
             const bool in = kb + row < len;
-            set_lds_chunk<E>(vs + LG::at(row, ch),
-                             load_chunk<E, DIRECT>(v0 + (in ? kb + row : 0) * p.v.token + 8 * ch,
-                                                   p.dv - 8 * ch, in, p.dv));
+            LG::store(vs + row / 32 * LG::kBytes, row % 32, ch,
+                      load_chunk<E, DIRECT>(v0 + (in ? kb + row : 0) * p.v.token + 8 * ch,
+                                            p.dv - 8 * ch, in, p.dv));
         }
     } else {
         const T *src = at<E>(p.v, w, kvh, live ? key : 0);
 #pragma unroll
         for (int i = 0; i < DV / 16; ++i)
-            v[i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
+            v[i] = as_frag(load_chunk<E, DIRECT>(src + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
                                                     live, p.dv));
     }
     f16v gk[2][DK / 32] = {}, gv[DV / 32] = {};
@@ -198,15 +196,15 @@ diff_dkv_kernel(DiffProblem p)
             for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
                 for (int a = 0; a < 2; ++a)
-                    s[a] = mma(row_frag<E>(qrow + a * kMap, i), k[a][i], s[a]);
+                    s[a] = mma(row_frag<E, DK>(qrow + a * kMap, i), k[a][i], s[a]);
             part();
 #pragma unroll
             for (int i = 0; i < DV / 16; ++i) {
                 if constexpr (kLdsV)
-                    x = mma(row_frag<E>(grow, i),
-                            row_frag<E>(first_row<E, DV>(vs + wave * 32 * LG::pitch), i), x);
+                    x = mma(row_frag<E, DV>(grow, i),
+                            row_frag<E, DV>(first_row<E, DV>(vs + wave * LG::kBytes), i), x);
                 else
-                    x = mma(row_frag<E>(grow, i), v[i], x);
+                    x = mma(row_frag<E, DV>(grow, i), v[i], x);
             }
             part();
         }

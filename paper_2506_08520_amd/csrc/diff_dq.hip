@@ -10,12 +10,16 @@ using namespace diff;
 
 // Sum of the products of eight elements and eight fp32 values.
 template <class E>
-__device__ inline float dot8(const Frag<E> &a, const Chunk<F32> &b)
+__device__ inline float dot8(const Chunk<E> &a, const Chunk<F32> &b)
 {
     float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        s = fmaf(float(a.x[j]), __uint_as_float(b.w[j]), s);
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t u = E::bytes == 4 ? a.w[j * E::bytes / 4]
+                           : j & 1       ? a.w[j / 2] & 0xffff0000u
+                                         : a.w[j / 2] << 16;
+        s = fmaf(__uint_as_float(u), __uint_as_float(b.w[j]), s);
+    }
     return s;
 }
 
@@ -27,7 +31,7 @@ __device__ inline float dot8(const Frag<E> &a, const Chunk<F32> &b)
 // at 4096 keys where rounding it alone costs 0.0017), or, where it kept none (few keys), from
 // a first walk over the keys.
 template <class E, int DK, int DV, int NW, bool DIRECT, bool KEPT>
-__global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>(!KEPT)))
+__global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>(!KEPT || E::bytes == 4)))
 diff_dq_kernel(DiffProblem p)
 {
     using T = typename E::T;
@@ -36,9 +40,9 @@ diff_dq_kernel(DiffProblem p)
     __shared__ alignas(256) char lds[2 * Tiles::kBuffer];
     const uint32_t buf = lds_offset(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
-    const int64_t b = xcd_order(blockIdx.x, gridDim.x);
-    const int tile = int(b % p.tiles);
-    const int64_t unit = b / p.tiles;
+    const Place here = place(p, blockIdx.x, gridDim.x, p.tiles, 1, true);
+    const int64_t unit = here.unit;
+    const int tile = here.tile;
     const int w = int(unit / p.G), kvh = int(unit % p.G);
     const int nrows = p.R * p.nq;
     const int r0 = tile * 32 * NW, r = r0 + wave * 32 + c;
@@ -61,7 +65,7 @@ diff_dq_kernel(DiffProblem p)
         const T *src = at<E>(p.q, w, 2 * row.head + a, row.token);
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
-            q[a][i] = as_frag<E>(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
+            q[a][i] = as_frag(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
                                                        p.d - 16 * i - 8 * g, live, p.d));
         const float2 sum = sum_row(p, w, row)[a * p.nq];
         base[a] = limit > 0 ? sum.x : INFINITY;   // exp2(-inf) = 0 where no key is seen
@@ -70,7 +74,7 @@ diff_dq_kernel(DiffProblem p)
     const T *gosrc = at<E>(p.go, w, row.head, row.token);
 #pragma unroll
     for (int i = 0; i < DV / 16; ++i)
-        go[i] = as_frag<E>(load_chunk<E, DIRECT>(gosrc + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
+        go[i] = as_frag(load_chunk<E, DIRECT>(gosrc + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
                                                  live, p.dv));
     if constexpr (KEPT) {
         const float *o2 = map_row<E>(p, w, row);
@@ -78,7 +82,7 @@ diff_dq_kernel(DiffProblem p)
 #pragma unroll 2   // more would hold more of the rows at once than there are registers
         for (int col = 8 * g; col < p.dv; col += 16) {
             const int n = p.dv - col;
-            const Frag<E> x = as_frag<E>(load_chunk<E, DIRECT>(gosrc + col, n, live, p.dv));
+            const Chunk<E> x = load_chunk<E, DIRECT>(gosrc + col, n, live, p.dv);
             D[0] += dot8(x, load_chunk<F32, false>(o1 + col, n, live, p.dv));
             D[1] += dot8(x, load_chunk<F32, false>(o2 + col, n, live, p.dv));
         }
@@ -104,17 +108,17 @@ diff_dq_kernel(DiffProblem p)
             if (__any(key < limit)) {
                 const uint32_t krow = first_row<E, DK>(t), kcol = first_col<E, DK>(t);
                 const uint32_t vrow = first_row<E, DV>(t + Tiles::kV);
-                constexpr uint32_t kMap = KT * Tiles::LK::pitch;
+                constexpr uint32_t kMap = Tiles::LK::kBytes;
                 f16v s[2] = {}, x = {};
 #pragma unroll
                 for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
                     for (int a = 0; a < 2; ++a)
-                        s[a] = mma(row_frag<E>(krow + a * kMap, i), q[a][i], s[a]);
+                        s[a] = mma(row_frag<E, DK>(krow + a * kMap, i), q[a][i], s[a]);
                 part();
 #pragma unroll
                 for (int i = 0; i < DV / 16; ++i)
-                    x = mma(row_frag<E>(vrow, i), go[i], x);
+                    x = mma(row_frag<E, DV>(vrow, i), go[i], x);
                 part();
                 if (!__all(key + KT <= limit)) {
                     hide(s[0], limit, key, g);

@@ -148,7 +148,7 @@ struct DiffProblem {
 
     uint32_t nq_mul;       // division by nq
     int nq_shift;
-    bool store_o, vec_gq, vec_gk, vec_gv;
+    bool even, store_o, vec_gq, vec_gk, vec_gv;
     int tiles, ktiles, splits, chunk, rsplits, rchunk, d4, dv4, partial_row;
     int64_t rows32;        // rows of a unit, up to a multiple of 32
     float *partial, *rows_lam, *row_lambda;   // [units][rows32] the last
