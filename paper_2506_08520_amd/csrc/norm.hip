@@ -120,6 +120,20 @@ __device__ inline void row_sums(float (&s)[N], float *lds)
     }
 }
 
+// A lane's part of one row: column (c LPR + lane) VEC of chunk c.  Lanes behind the row load
+// its start again; what they hold is dropped where it is used.
+template <class E, int VEC, int LPR, int CH>
+__device__ inline void load_row(const typename E::T *row, int C, Raw<E, VEC> (&x)[CH])
+{
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * LPR + threadIdx.x % LPR) * VEC;
+        x[c] = load_raw<E, VEC>(row + (col < C ? col : 0));
+    }
+}
+
+// Workgroup `blockIdx.x` takes the row groups blockIdx.x, + gridDim.x, ..., the next one's
+// loads ahead of the work on one, with weight and bias in registers.
 template <class E, int VEC, int LPR, int CH>
 __global__ void __launch_bounds__(kThreads)
 norm_forward_kernel(NormProblem p)
@@ -128,65 +142,73 @@ norm_forward_kernel(NormProblem p)
     __shared__ float lds[8];
     constexpr int kRows = kThreads / LPR;
     const int lane = threadIdx.x % LPR;
-    const int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LPR;
-    const bool live = row < p.rows;
-    const T *x = static_cast<const T *>(p.x) + (live ? row : 0) * p.x_stride;
-    float v[CH][VEC];
-    float s[1] = {0.f};
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int col = (c * LPR + lane) * VEC;
-        if (live && col < p.C) {
-            load_vec<E, VEC>(x + col, v[c]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                v[c][j] = 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-            s[0] += v[c][j];
-    }
-    row_sums<LPR>(s, lds);
-    const float mean = s[0] / float(p.C);
-    s[0] = 0.f;
+    float w[CH][VEC], b[CH][VEC];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * LPR + lane) * VEC;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            v[c][j] = col < p.C ? v[c][j] - mean : 0.f;
-            s[0] = fmaf(v[c][j], v[c][j], s[0]);
+            w[c][j] = 1.f;
+            b[c][j] = 0.f;
         }
+        if (p.w && col < p.C)
+            load_vec<E, VEC>(static_cast<const T *>(p.w) + col, w[c]);
+        if (p.b && col < p.C)
+            load_vec<E, VEC>(static_cast<const T *>(p.b) + col, b[c]);
     }
-    row_sums<LPR>(s, lds);
-    const float rstd = 1.f / sqrtf(s[0] / float(p.C) + p.eps);
-    if (!live)
-        return;
-    T *y = static_cast<T *>(p.y) + row * p.y_stride;
+    const int64_t step = int64_t(gridDim.x) * kRows;
+    int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / LPR;
+    const float inv = 1.f / float(p.C);
+    Raw<E, VEC> next[CH];
+    const T *x = static_cast<const T *>(p.x);
+    load_row<E, VEC, LPR, CH>(x + (row < p.rows ? row : 0) * p.x_stride, p.C, next);
+    for (int64_t r0 = int64_t(blockIdx.x) * kRows; r0 < p.rows; r0 += step, row += step) {
+        float v[CH][VEC];
+        float s[1] = {0.f};
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int col = (c * LPR + lane) * VEC;
-        if (col < p.C) {
-            float w[VEC], b[VEC];
+        for (int c = 0; c < CH; ++c) {
+            const bool in = (c * LPR + lane) * VEC < p.C;
+            unpack<E, VEC>(next[c], v[c]);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                w[j] = 1.f;
-                b[j] = 0.f;
+                v[c][j] = in ? v[c][j] : 0.f;
+                s[0] += v[c][j];
             }
-            if (p.w)
-                load_vec<E, VEC>(static_cast<const T *>(p.w) + col, w);
-            if (p.b)
-                load_vec<E, VEC>(static_cast<const T *>(p.b) + col, b);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                v[c][j] = fmaf(v[c][j] * rstd, w[j], b[j]);
-            store_vec<E, VEC>(y + col, v[c]);
         }
-    }
-    if (lane == 0 && p.mean) {
-        p.mean[row] = mean;
-        p.rstd[row] = rstd;
+        if (r0 + step < p.rows)
+            load_row<E, VEC, LPR, CH>(x + (row + step < p.rows ? row + step : 0) * p.x_stride,
+                                      p.C, next);
+        row_sums<LPR>(s, lds);
+        const float mean = s[0] / float(p.C);   // divided: equal values have no deviation
+        s[0] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const bool in = (c * LPR + lane) * VEC < p.C;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                v[c][j] = in ? v[c][j] - mean : 0.f;
+                s[0] = fmaf(v[c][j], v[c][j], s[0]);
+            }
+        }
+        row_sums<LPR>(s, lds);
+        const float rstd = 1.f / sqrtf(s[0] * inv + p.eps);
+        if (row < p.rows) {
+            T *y = static_cast<T *>(p.y) + row * p.y_stride;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = (c * LPR + lane) * VEC;
+                if (col < p.C) {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        v[c][j] = fmaf(v[c][j] * rstd, w[c][j], b[c][j]);
+                    store_vec<E, VEC>(y + col, v[c]);
+                }
+            }
+            if (lane == 0 && p.mean) {
+                p.mean[row] = mean;
+                p.rstd[row] = rstd;
+            }
+        }
     }
 }
 
@@ -216,6 +238,7 @@ norm_backward_kernel(NormProblem p, float *partial)
     }
     // The rows are fetched one ahead: with few rows to a workgroup it is the latency of
     // their loads that bounds it.
+    const float inv = 1.f / float(p.C);
     const int64_t step = int64_t(gridDim.x) * kRows;
     int64_t row = int64_t(blockIdx.x) * kRows + group;
     Raw<E, VEC> xn[CH], gn[CH];
@@ -226,13 +249,8 @@ norm_backward_kernel(NormProblem p, float *partial)
         const T *dy = static_cast<const T *>(p.dy) + rr * p.dy_stride;
         mean_n = p.mean[rr];
         rstd_n = p.rstd[rr];
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            // Lanes behind the row load its start again, and drop it below.
-            const int col = (c * LPR + lane) * VEC;
-            xn[c] = load_raw<E, VEC>(x + (col < p.C ? col : 0));
-            gn[c] = load_raw<E, VEC>(dy + (col < p.C ? col : 0));
-        }
+        load_row<E, VEC, LPR, CH>(x, p.C, xn);
+        load_row<E, VEC, LPR, CH>(dy, p.C, gn);
     };
     fetch(row);
     for (int64_t r0 = int64_t(blockIdx.x) * kRows; r0 < p.rows; r0 += step, row += step) {
@@ -264,7 +282,7 @@ norm_backward_kernel(NormProblem p, float *partial)
                 s[1] = fmaf(g[c][j], xh[c][j], s[1]);
             }
         row_sums<LPR>(s, lds);
-        const float m0 = s[0] / float(p.C), m1 = s[1] / float(p.C);
+        const float m0 = s[0] * inv, m1 = s[1] * inv;
         if (live) {
             T *dx = static_cast<T *>(p.dx) + row * p.dx_stride;
 #pragma unroll
@@ -388,10 +406,25 @@ void launch(const NormProblem &p, float *partial, int groups, hipStream_t s)
     if (partial) {
         norm_backward_kernel<E, VEC, LPR, CH><<<groups, kThreads, 0, s>>>(p, partial);
     } else {
-        const int64_t per = kThreads / LPR;
+        // At most eight workgroups to a CU.
+        const int64_t per = kThreads / LPR, blocks = (p.rows + per - 1) / per;
         norm_forward_kernel<E, VEC, LPR, CH>
-            <<<dim3(unsigned((p.rows + per - 1) / per)), kThreads, 0, s>>>(p);
+            <<<dim3(unsigned(blocks < 2048 ? blocks : 2048)), kThreads, 0, s>>>(p);
     }
+}
+
+// A lane holds 8, 12 or 16 values, the fewest that do (12 not of wide loads, which they
+// cannot be made of).
+template <class E, int VEC, int LPR>
+void launch_lanes(const NormProblem &p, float *partial, int groups, hipStream_t s)
+{
+    if (p.C <= 8 * LPR)
+        return launch<E, VEC, LPR, 8>(p, partial, groups, s);
+    if constexpr (12 % VEC == 0) {
+        if (p.C <= 12 * LPR)
+            return launch<E, VEC, LPR, 12>(p, partial, groups, s);
+    }
+    launch<E, VEC, LPR, 16>(p, partial, groups, s);
 }
 
 // At most 16 values a lane: 16 lanes hold a row of up to 256 channels (four
@@ -400,16 +433,12 @@ template <class E, int VEC>
 void launch_vec(const NormProblem &p, float *partial, int groups, hipStream_t s)
 {
     const int lanes = lanes_per_row(p.C);
-    const bool half = p.C <= 8 * lanes;
     if (lanes == 16)
-        half ? launch<E, VEC, 16, 8>(p, partial, groups, s)
-             : launch<E, VEC, 16, 16>(p, partial, groups, s);
+        launch_lanes<E, VEC, 16>(p, partial, groups, s);
     else if (lanes == 64)
-        half ? launch<E, VEC, 64, 8>(p, partial, groups, s)
-             : launch<E, VEC, 64, 16>(p, partial, groups, s);
+        launch_lanes<E, VEC, 64>(p, partial, groups, s);
     else
-        half ? launch<E, VEC, 256, 8>(p, partial, groups, s)
-             : launch<E, VEC, 256, 16>(p, partial, groups, s);
+        launch_lanes<E, VEC, 256>(p, partial, groups, s);
 }
 
 void launch_any(const NormProblem &p, float *partial, int groups, hipStream_t s)
