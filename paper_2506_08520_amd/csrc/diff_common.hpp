@@ -248,9 +248,8 @@ struct Tile {
 // Row fragments: row lane % 32 of the tile at `tile`, contraction indices (columns)
 // 16 c + 8 g + j.  first_row() gives the address for c = 0.
 template <class E, int COLS>
-__device__ inline uint32_t first_row(uint32_t tile)
+__device__ inline uint32_t first_row(uint32_t tile, unsigned lane = threadIdx.x & 63)
 {
-    const int lane = threadIdx.x & 63;
     return tile + Tile<E, COLS>::at(lane & 31, lane >> 5);
 }
 
@@ -270,9 +269,8 @@ __device__ inline Frag<E> row_frag(uint32_t first, int c)
 // of 16 columns from 16 lanes (lane p: row p / 4, columns 4 (p % 4) ..) and gives each lane
 // its column of them.
 template <class E, int COLS>
-__device__ inline uint32_t first_col(uint32_t tile)
+__device__ inline uint32_t first_col(uint32_t tile, unsigned lane = threadIdx.x & 63)
 {
-    const int lane = threadIdx.x & 63;
     const int col = (lane & 16) + 4 * (lane & 3);
     return tile + Tile<E, COLS>::at(4 * (lane >> 5) + ((lane & 15) >> 2), col >> 3) +
            2 * (col & 7);
@@ -349,22 +347,33 @@ __device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t l
 
 __device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// The thread's number, worked out anew by everything that follows from it here: for kernels
+// that have no registers to keep such values in from one tile to the next (where they went to
+// memory, their loads waited for the tile's).
+__device__ inline unsigned thread_again()
+{
+    unsigned thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    return thread;
+}
+
 // The same tile by loads that go to LDS directly, for rows of whole 16-byte chunks; at(row)
 // is the row's offset from `base` in elements, below 2^30.  Every lane loads: rows that are
 // not there must be given as another's (their products are masked), and columns from `cols`
 // on hold the last chunk again (the other operand is zero there).
 template <int COLS, int ROWS, int NT, class At>
-__device__ inline void direct_tile(uint32_t lds, const void *base, At at, int cols)
+__device__ inline void direct_tile(uint32_t lds, const void *base, At at, int cols,
+                                   unsigned thread = threadIdx.x)
 {
     using L = Tile<BF16, COLS>;
     static_assert(ROWS * L::kRow % NT == 0, "whole waves");
+    const uint32_t to = lds + 1024 * __builtin_amdgcn_readfirstlane(thread / 64);
 #pragma unroll
     for (int i = 0; i < ROWS * L::kRow / NT; ++i) {
-        const int id = threadIdx.x + i * NT;
-        const int row = id / L::kRow, chunk = id % L::kRow ^ L::swap(row);
+        const unsigned id = thread + i * NT;
+        const int row = id / L::kRow, chunk = int(id % L::kRow) ^ L::swap(row);
         const int col = min(8 * chunk, cols - 8);
-        load_to_lds(base, 2 * uint32_t(at(row) + col),
-                    __builtin_amdgcn_readfirstlane(lds + 16 * (i * NT + (threadIdx.x & ~63u))));
+        load_to_lds(base, 2 * uint32_t(at(row) + col), to + 16 * i * NT);
     }
 }
 

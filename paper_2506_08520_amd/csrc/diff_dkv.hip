@@ -136,8 +136,10 @@ diff_dkv_kernel(DiffProblem p)
     auto fetch = [&](int r0, uint32_t t) {
         if constexpr (DIRECT) {
             direct_tile<DK, 2 * QT, NT>(
-                t, q0, [&](int i) { return q_row(r0 + i % QT, i / QT); }, p.d);
-            direct_tile<DV, QT, NT>(t + kGo, go0, [&](int i) { return go_row(r0 + i); }, p.dv);
+                t, q0, [&](int i) { return q_row(r0 + i % QT, i / QT); }, p.d,
+                thread_again());
+            direct_tile<DV, QT, NT>(
+                t + kGo, go0, [&](int i) { return go_row(r0 + i); }, p.dv, thread_again());
         } else {
             sq.load([&](int i) { return q0 + q_row(r0 + i % QT, i / QT); },
                     [&](int i) { return r0 + i % QT < nrows; }, p.d);
@@ -190,8 +192,9 @@ diff_dkv_kernel(DiffProblem p)
         const bool any = __any(kw < rowlim), masked = p.causal && !__all(kw + 32 <= rowlim);
         f16v s[2] = {}, x = {};
         if (any) {
-            const uint32_t qrow = first_row<E, DK>(t);
-            const uint32_t grow = first_row<E, DV>(t + kGo);
+            const unsigned at_lane = thread_again() & 63;
+            const uint32_t qrow = first_row<E, DK>(t, at_lane);
+            const uint32_t grow = first_row<E, DV>(t + kGo, at_lane);
 #pragma unroll
             for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
@@ -202,7 +205,7 @@ diff_dkv_kernel(DiffProblem p)
             for (int i = 0; i < DV / 16; ++i) {
                 if constexpr (kLdsV)
                     x = mma(row_frag<E, DV>(grow, i),
-                            row_frag<E, DV>(first_row<E, DV>(vs + wave * LG::kBytes), i), x);
+                            row_frag<E, DV>(first_row<E, DV>(vs + wave * LG::kBytes, at_lane), i), x);
                 else
                     x = mma(row_frag<E, DV>(grow, i), v[i], x);
             }
@@ -213,7 +216,9 @@ diff_dkv_kernel(DiffProblem p)
         if (r1 < rend)
             fetch(r1, other);
         if (any) {
-            const uint32_t qcol = first_col<E, DK>(t), gcol = first_col<E, DV>(t + kGo);
+            const unsigned at_lane = thread_again() & 63;
+            const uint32_t qcol = first_col<E, DK>(t, at_lane);
+            const uint32_t gcol = first_col<E, DV>(t + kGo, at_lane);
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -236,6 +241,7 @@ diff_dkv_kernel(DiffProblem p)
                     s[0][i] = p1 * (x[i] - st.z);
                     s[1][i] = p2 * (st.w - x[i]);
                 }
+                part();
             }
             if (masked) {
 #pragma unroll
