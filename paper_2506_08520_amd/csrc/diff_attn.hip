@@ -23,8 +23,8 @@ diff_forward_kernel(DiffProblem p)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
     const Place here = place(p, blockIdx.x, gridDim.x, p.tiles, p.splits, true);
     const int64_t unit = here.unit;
+    const int w = int(here.unit / unsigned(p.G)), kvh = int(here.unit) - w * p.G;
     const int tile = here.tile, split = here.split;
-    const int w = int(unit / p.G), kvh = int(unit % p.G);
     const int nrows = p.R * p.nq;
     const int r0 = tile * 32 * NW, r = r0 + wave * 32 + c;
     const bool live = r < nrows;
@@ -105,11 +105,7 @@ diff_forward_kernel(DiffProblem p)
         for (int a = 0; a < 2; ++a) {
 #pragma unroll
             for (int i = 0; i < DV / 32; ++i)
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    store4<F32>(out + a * p.dv4, 32 * i + 8 * t + 4 * g, p.dv4, true,
-                                acc[a][i][4 * t], acc[a][i][4 * t + 1], acc[a][i][4 * t + 2],
-                                acc[a][i][4 * t + 3]);
+                store_block<F32>(out + a * p.dv4, i, g, p.dv4, true, acc[a][i]);
             if (g == 0) {
                 out[2 * p.dv4 + 2 * a] = m[a];
                 out[2 * p.dv4 + 2 * a + 1] = l[a];
@@ -122,26 +118,23 @@ diff_forward_kernel(DiffProblem p)
     const float lam = p.lambda[row.head];
     T *o = at_out<E>(p.o, w, row.head, row.token);
     float *maps = p.maps ? map_row<E>(p, w, row) : nullptr;
+    const bool maps4 = p.dv % 4 == 0;
 #pragma unroll
-    for (int i = 0; i < DV / 32; ++i)
+    for (int i = 0; i < DV / 32; ++i) {
+        f16v &x = acc[0][i], &y = acc[1][i], o16;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            float x[4], y[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[j] = acc[0][i][4 * t + j] * inv1;
-                y[j] = acc[1][i][4 * t + j] * inv2;
-            }
-            const int col = 32 * i + 8 * t + 4 * g;
-            store4<E>(o, col, p.dv, p.store_o, difference(x[0], lam, y[0]),
-                      difference(x[1], lam, y[1]), difference(x[2], lam, y[2]),
-                      difference(x[3], lam, y[3]));
-            if (maps) {
-                store4<F32>(maps, col, p.dv, p.dv % 4 == 0, y[0], y[1], y[2], y[3]);
-                if (E::bytes == 2)
-                    store4<F32>(maps + p.dv, col, p.dv, p.dv % 4 == 0, x[0], x[1], x[2], x[3]);
-            }
+        for (int r = 0; r < 16; ++r) {
+            x[r] *= inv1;
+            y[r] *= inv2;
+            o16[r] = difference(x[r], lam, y[r]);
         }
+        store_block<E>(o, i, g, p.dv, p.store_o, o16);
+        if (maps) {
+            store_block<F32>(maps, i, g, p.dv, maps4, y);
+            if (E::bytes == 2)
+                store_block<F32>(maps + p.dv, i, g, p.dv, maps4, x);
+        }
+    }
     if (p.sums && g == 0) {
         float2 *sums = sum_row(p, w, row);
         sums[0] = make_float2(m[0], l[0]);
@@ -158,11 +151,12 @@ diff_merge_few_kernel(DiffProblem p, int64_t items)
     if (item >= items)
         return;
     const int nrows = p.R * p.nq, groups = p.dv4 / 4;
-    const int64_t at_row = item / groups;
-    const int col = int(item - at_row * groups) * 4;
-    const int64_t unit = at_row / nrows;
-    const int r = int(at_row - unit * nrows);
-    const int w = int(unit / p.G), kvh = int(unit % p.G);
+    // below 2^24 rows of at most 32 groups
+    const unsigned at_row = unsigned(item) / unsigned(groups);
+    const int col = int(unsigned(item) - at_row * groups) * 4;
+    const int64_t unit = at_row / unsigned(nrows);
+    const int r = int(at_row - unsigned(unit) * nrows);
+    const int w = int(unsigned(unit) / unsigned(p.G)), kvh = int(unit) - w * p.G;
     const Row row = row_of(p, kvh, r);
     const float *part = p.partial + (unit * p.splits * nrows + r) * p.partial_row;
     const int64_t step = int64_t(nrows) * p.partial_row;
@@ -190,14 +184,16 @@ diff_merge_few_kernel(DiffProblem p, int64_t items)
     for (int a = 0; a < 2; ++a)
         x[a] *= l[a] == 0.f ? 0.f : 1.f / l[a];
     const float lam = p.lambda[row.head];
-    store4<E>(at_out<E>(p.o, w, row.head, row.token), col, p.dv, p.store_o,
-              difference(x[0][0], lam, x[1][0]), difference(x[0][1], lam, x[1][1]),
-              difference(x[0][2], lam, x[1][2]), difference(x[0][3], lam, x[1][3]));
+    f4 o;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        o[j] = difference(x[0][j], lam, x[1][j]);
+    store4<E>(at_out<E>(p.o, w, row.head, row.token), col, p.dv, p.store_o, o);
     if (p.maps) {
         float *maps = map_row<E>(p, w, row);
-        store4<F32>(maps, col, p.dv, p.dv % 4 == 0, x[1][0], x[1][1], x[1][2], x[1][3]);
+        store4<F32>(maps, col, p.dv, p.dv % 4 == 0, x[1]);
         if (E::bytes == 2)
-            store4<F32>(maps + p.dv, col, p.dv, p.dv % 4 == 0, x[0][0], x[0][1], x[0][2], x[0][3]);
+            store4<F32>(maps + p.dv, col, p.dv, p.dv % 4 == 0, x[0]);
     }
     if (p.sums && col == 0) {
 #pragma unroll
@@ -217,7 +213,7 @@ diff_merge_kernel(DiffProblem p)
     const int nrows = p.R * p.nq;
     const int64_t unit = blockIdx.x / unsigned(nrows);
     const int r = int(blockIdx.x - unit * nrows);
-    const int w = int(unit / p.G), kvh = int(unit % p.G);
+    const int w = int(unsigned(unit) / unsigned(p.G)), kvh = int(unit) - w * p.G;
     const Row row = row_of(p, kvh, r);
     const float *part = p.partial + (unit * p.splits * nrows + r) * p.partial_row;
     const int64_t step = int64_t(nrows) * p.partial_row;

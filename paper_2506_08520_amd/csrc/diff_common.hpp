@@ -460,24 +460,27 @@ __device__ inline typename E::T *at_out(const DiffView &v, int64_t w, int64_t he
     return static_cast<typename E::T *>(v.data) + w * v.window + head * v.head + token * v.token;
 }
 
+template <class E>
+__device__ inline void store_vec4(typename E::T *at, f4 x)
+{
+    if constexpr (E::bytes == 4) {
+        *reinterpret_cast<f4 *>(at) = x;
+    } else {
+        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<b4 *>(at) = __builtin_convertvector(x, b4);   // to nearest even
+    }
+}
+
 // Four consecutive elements of an output row from column `col`, those below `n`; `vec`
 // says that such groups are whole and aligned.
 template <class E>
-__device__ inline void store4(typename E::T *row, int col, int n, bool vec, float a, float b,
-                              float c, float d)
+__device__ inline void store4(typename E::T *row, int col, int n, bool vec, f4 x)
 {
     if (vec) {
-        if (col < n) {
-            if constexpr (E::bytes == 4) {
-                *reinterpret_cast<float4 *>(row + col) = make_float4(a, b, c, d);
-            } else {
-                typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-                *reinterpret_cast<b4 *>(row + col) = __builtin_convertvector((f4{a, b, c, d}), b4);
-            }
-        }
+        if (col < n)
+            store_vec4<E>(row + col, x);
         return;
     }
-    const float x[4] = {a, b, c, d};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (col + j < n) {
@@ -486,6 +489,29 @@ __device__ inline void store4(typename E::T *row, int col, int n, bool vec, floa
             else
                 reinterpret_cast<__bf16 *>(row)[col + j] = __bf16(x[j]);
         }
+}
+
+// A lane's part of the columns 32 i .. 32 i + 31 of its output row, times `scale`: in the order
+// of a product's result, 32 i + 8 (r / 4) + 4 g + r % 4.
+template <class E>
+__device__ inline void store_block(typename E::T *row, int i, int g, int n, bool vec,
+                                   const f16v &x, float scale = 1.f)
+{
+    f4 v[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[t][j] = scale * x[4 * t + j];
+    if (vec && 32 * i + 32 <= n) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            store_vec4<E>(row + 4 * g + 32 * i + 8 * t, v[t]);
+    } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            store4<E>(row, 32 * i + 8 * t + 4 * g, n, vec, v[t]);
+    }
 }
 
 // The exponents' base and the sum of a row's exponentials for its first map, in
@@ -560,31 +586,33 @@ __device__ inline void softmax_step(f16v &s, float scale2, float &m, float &l, G
 // fetched into one L2 only.  Uneven work (causal masks, lengths): the tiles with the most
 // keys of all units first, over all XCDs.
 struct Place {
-    int64_t unit;
+    unsigned unit;
     int tile, split;
 };
 
-__device__ inline Place place(const DiffProblem &p, int64_t b, int64_t n, int tiles, int splits,
-                              bool last_first)
+// All in 32 bits (a launch has fewer than 2^24 workgroups): a division of 64 bits is over a
+// hundred instructions.
+__device__ inline Place place(const DiffProblem &p, unsigned b, unsigned n, unsigned tiles,
+                              unsigned splits, bool last_first)
 {
-    Place at;
+    unsigned unit, tile, split;
     if (p.even) {
-        const int64_t per = n / 8, full = per * 8;
+        const unsigned per = n / 8, full = per * 8;
         b = b < full ? (b % 8) * per + b / 8 : b;
-        at.split = int(b % splits);
-        b /= splits;
-        at.tile = int(b % tiles);
-        at.unit = b / tiles;
+        const unsigned rest = b / splits;
+        split = b - rest * splits;
+        unit = rest / tiles;
+        tile = rest - unit * tiles;
     } else {
-        const int64_t units = int64_t(p.W) * p.G;
-        at.unit = b % units;
-        b /= units;
-        at.split = int(b % splits);
-        at.tile = int(b / splits);
+        const unsigned units = unsigned(p.W) * unsigned(p.G);
+        const unsigned rest = b / units;
+        unit = b - rest * units;
+        tile = rest / splits;
+        split = rest - tile * splits;
         if (last_first)
-            at.tile = tiles - 1 - at.tile;
+            tile = tiles - 1 - tile;
     }
-    return at;
+    return Place{unit, int(tile), int(split)};
 }
 
 // Keys and values of a unit, tile after tile of KT keys, into two LDS buffers in turn:

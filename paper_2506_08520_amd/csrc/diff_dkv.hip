@@ -74,8 +74,8 @@ diff_dkv_kernel(DiffProblem p)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
     const Place here = place(p, blockIdx.x - p.H, gridDim.x - p.H, p.ktiles, p.rsplits, false);
     const int64_t unit = here.unit;
+    const int w = int(here.unit / unsigned(p.G)), kvh = int(here.unit) - w * p.G;
     const int tile = here.tile, split = here.split;
-    const int w = int(unit / p.G), kvh = int(unit % p.G);
     const int nrows = p.R * p.nq;
     const int kb = tile * 32 * NW, kw = kb + wave * 32, key = kw + c;
     const int len = window_len(p, w);
@@ -277,44 +277,35 @@ diff_dkv_kernel(DiffProblem p)
     if (p.rsplits > 1) {
         float *out = p.partial + ((unit * p.rsplits + split) * p.nk + key) * p.partial_row;
 #pragma unroll
-        for (int i = 0; i < DK / 32; ++i)
+        for (int a = 0; a < 2; ++a)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int a = 0; a < 2; ++a)
-                    store4<F32>(out + a * p.d4, 32 * i + 8 * j + 4 * g, p.d4, true,
-                                gk[a][i][4 * j], gk[a][i][4 * j + 1], gk[a][i][4 * j + 2],
-                                gk[a][i][4 * j + 3]);
+            for (int i = 0; i < DK / 32; ++i)
+                store_block<F32>(out + a * p.d4, i, g, p.d4, true, gk[a][i]);
 #pragma unroll
         for (int i = 0; i < DV / 32; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                store4<F32>(out + 2 * p.d4, 32 * i + 8 * j + 4 * g, p.dv4, true, gv[i][4 * j],
-                            gv[i][4 * j + 1], gv[i][4 * j + 2], gv[i][4 * j + 3]);
+            store_block<F32>(out + 2 * p.d4, i, g, p.dv4, true, gv[i]);
         return;
+    }
+    // Keys behind the length, whose operands were zeros, have gradients of zero, but for NaN
+    // that a query brought in.
+    if (!live) {
+#pragma unroll
+        for (int i = 0; i < DV / 32; ++i)
+            gv[i] = f16v{};
+#pragma unroll
+        for (int i = 0; i < DK / 32; ++i)
+            gk[0][i] = gk[1][i] = f16v{};
     }
     const float scale = key_scale(p, len);
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
-        T *dst = at_out<E>(p.gk, w, 2 * kvh + a, key);
+    for (int a = 0; a < 2; ++a)
 #pragma unroll
         for (int i = 0; i < DK / 32; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                store4<E>(dst, 32 * i + 8 * j + 4 * g, p.d, p.vec_gk,
-                          live ? scale * gk[a][i][4 * j] : 0.f,
-                          live ? scale * gk[a][i][4 * j + 1] : 0.f,
-                          live ? scale * gk[a][i][4 * j + 2] : 0.f,
-                          live ? scale * gk[a][i][4 * j + 3] : 0.f);
-    }
-    T *dst = at_out<E>(p.gv, w, kvh, key);
+            store_block<E>(at_out<E>(p.gk, w, 2 * kvh + a, key), i, g, p.d, p.vec_gk, gk[a][i],
+                           scale);
 #pragma unroll
     for (int i = 0; i < DV / 32; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            store4<E>(dst, 32 * i + 8 * j + 4 * g, p.dv, p.vec_gv, live ? gv[i][4 * j] : 0.f,
-                      live ? gv[i][4 * j + 1] : 0.f, live ? gv[i][4 * j + 2] : 0.f,
-                      live ? gv[i][4 * j + 3] : 0.f);
+        store_block<E>(at_out<E>(p.gv, w, kvh, key), i, g, p.dv, p.vec_gv, gv[i]);
 }
 
 // Adds up the row ranges of one key.
@@ -324,7 +315,7 @@ diff_dkv_merge_kernel(DiffProblem p)
 {
     const int64_t unit = blockIdx.x / unsigned(p.nk);
     const int key = int(blockIdx.x - unit * p.nk);
-    const int w = int(unit / p.G), kvh = int(unit % p.G);
+    const int w = int(unsigned(unit) / unsigned(p.G)), kvh = int(unit) - w * p.G;
     const int len = window_len(p, w);
     const bool live = key < len;
     const float scale = key_scale(p, len);

@@ -42,8 +42,8 @@ diff_dq_kernel(DiffProblem p)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
     const Place here = place(p, blockIdx.x, gridDim.x, p.tiles, 1, true);
     const int64_t unit = here.unit;
+    const int w = int(here.unit / unsigned(p.G)), kvh = int(here.unit) - w * p.G;
     const int tile = here.tile;
-    const int w = int(unit / p.G), kvh = int(unit % p.G);
     const int nrows = p.R * p.nq;
     const int r0 = tile * 32 * NW, r = r0 + wave * 32 + c;
     const bool live = r < nrows;
@@ -184,11 +184,7 @@ diff_dq_kernel(DiffProblem p)
         T *dst = at_out<E>(p.gq, w, 2 * row.head + a, row.token);
 #pragma unroll
         for (int i = 0; i < DK / 32; ++i)
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                store4<E>(dst, 32 * i + 8 * t + 4 * g, p.d, p.vec_gq, scale * acc[a][i][4 * t],
-                          scale * acc[a][i][4 * t + 1], scale * acc[a][i][4 * t + 2],
-                          scale * acc[a][i][4 * t + 3]);
+            store_block<E>(dst, i, g, p.d, p.vec_gq, acc[a][i], scale);
     }
 }
 
