@@ -406,7 +406,7 @@ typedef enum {
     NYSTRA_CAUSAL_END = 2
 } nystra_causal;
 
-#define NYSTRA_DIFF_SHORT_KEYS 128
+#define NYSTRA_DIFF_SHORT_KEYS 256
 
 typedef struct nystra_view {
     void *data;

@@ -33,7 +33,7 @@ EXPORTS = (
 STATIC_SCRATCH_BYTES = 32 << 20   # NYSTRA_STATIC_SCRATCH_BYTES
 BLOCK_NYSTROM, BLOCK_EXACT = 0, 1
 CAUSAL_NONE, CAUSAL_START, CAUSAL_END = 0, 1, 2
-DIFF_SHORT_KEYS = 128             # NYSTRA_DIFF_SHORT_KEYS
+DIFF_SHORT_KEYS = 256             # NYSTRA_DIFF_SHORT_KEYS
 
 
 class NystraError(RuntimeError):

@@ -78,7 +78,7 @@ def visible(W, nq, nk, causal, kv_len):
     return out
 
 
-def diff_attention(q, k, v, lam, causal=0, kv_len=None, scale=None, do=None, short=128):
+def diff_attention(q, k, v, lam, causal=0, kv_len=None, scale=None, do=None, short=256):
     """[(value, bound)] of O, and with do of dq, dk, dv, dlam.  Masked keys and values
     are left out, not multiplied by zero."""
     dt = q.dtype

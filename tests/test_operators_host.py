@@ -85,7 +85,7 @@ def test_dropout_refusals(L):
     assert drop(L, n=0, x=None, y=None) == OK
 
 
-def shape(W=2, H=4, G=2, nq=64, nk=200, d=30, dv=60, causal=0, scale=0.0):
+def shape(W=2, H=4, G=2, nq=64, nk=300, d=30, dv=60, causal=0, scale=0.0):
     return B.DiffShape(W, H, G, nq, nk, d, dv, causal, scale)
 
 
@@ -157,9 +157,9 @@ def test_diff_attention_saved_values(L):
     # many keys: both; few: the sums alone; inference: neither
     assert forward(L, sums=None) == ENULL
     assert forward(L, maps=None) == ENULL
-    assert forward(L, s=shape(nk=128)) == ENULL
+    assert forward(L, s=shape(nk=256)) == ENULL
     assert backward(L, maps=None) == ENULL and backward(L, sums=None) == ENULL
-    assert backward(L, s=shape(nk=128)) == ENULL
+    assert backward(L, s=shape(nk=256)) == ENULL
     assert backward(L, dlam=None) == ENULL and backward(L, dlam=A[11] + 1) == EALIGN
     assert forward(L, sums=A[3]) == EOVERLAP and forward(L, maps=A[0]) == EOVERLAP
     assert backward(L, dlam=A[5]) == EOVERLAP and backward(L, dlam=A[8]) == EOVERLAP
