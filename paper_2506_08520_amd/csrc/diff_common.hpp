@@ -136,18 +136,19 @@ __device__ inline Chunk<E> load_chunk(const typename E::T *p, int n, bool live, 
                     w[2] = w[2] >> 16 | w[3] << 16, w[3] >>= 16;
             }
         } else {
-#pragma unroll
+            w[0] = w[1] = w[2] = w[3] = 0u;
+#pragma unroll 1   // rare and called in many places: small code
             for (int j = 0; j < per; ++j) {
-                uint32_t u = 0;
-                if (E::bytes == 4)
-                    u = *reinterpret_cast<const uint32_t *>(p + h * per + min(j, left - 1));
-                else
-                    u = *reinterpret_cast<const uint16_t *>(p + h * per + min(j, left - 1));
-                u = j < left ? u : 0u;
-                if (E::bytes == 4)
-                    w[j] = u;
-                else
-                    w[j / 2] = j & 1 ? w[j / 2] | u << 16 : u;
+                // The next element in from the top, the others down by one.
+                const typename E::T *q = p + h * per + min(j, left - 1);
+                if (E::bytes == 4) {
+                    const uint32_t u = *reinterpret_cast<const uint32_t *>(q);
+                    w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = j < left ? u : 0u;
+                } else {
+                    const uint32_t u = *reinterpret_cast<const uint16_t *>(q);
+                    w[0] = w[0] >> 16 | w[1] << 16, w[1] = w[1] >> 16 | w[2] << 16;
+                    w[2] = w[2] >> 16 | w[3] << 16, w[3] = w[3] >> 16 | (j < left ? u << 16 : 0u);
+                }
             }
         }
 #pragma unroll
