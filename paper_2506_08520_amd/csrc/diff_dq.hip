@@ -39,6 +39,11 @@ diff_dq_kernel(DiffProblem p)
     using T = typename E::T;
     using Tiles = KeyTiles<E, DK, DV, 64 * NW, DIRECT>;
     constexpr int KT = Tiles::KT;
+    // The row's part of -dlam is dO . O_2 = D_2.  bf16 forms it here from the probabilities,
+    // where O_2 came from their roundings (323 keys: dlam off by 1.5e-3 from O_2, 4.8e-7 so).
+    // fp32 takes the kept O_2: the matrix instruction's sums round towards one side, which
+    // dO . V carries into every row alike (777 keys: 1.5e-6 from dO . V, 1.6e-7 so).
+    constexpr bool kSumLambda = KEPT && E::bytes == 2;
     __shared__ alignas(256) char lds[2 * Tiles::kBuffer];
     const uint32_t buf = lds_offset(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
@@ -96,7 +101,7 @@ diff_dq_kernel(DiffProblem p)
     }
     const float w1 = inv[0], w2 = -lam * inv[1];
     f16v acc[2][DK / 32] = {};
-    float glam = 0.f;
+    float glam = 0.f;   // bf16 with kept maps; D_2 where that is as exact
     if (kend > 0)
         tiles.commit(buf);
     uint32_t t = buf, other = buf + Tiles::kBuffer;   // this tile's buffer and the next one's
@@ -141,7 +146,8 @@ diff_dq_kernel(DiffProblem p)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         // the sums of the exponentials divide the other factor
-                        glam = fmaf(s[1][i], x[i], glam);
+                        if (kSumLambda)
+                            glam = fmaf(s[1][i], x[i], glam);
                         s[0][i] *= fmaf(w1, x[i], -w1 * D[0]);
                         s[1][i] *= fmaf(w2, x[i], -w2 * D[1]);
                     }
@@ -166,7 +172,7 @@ diff_dq_kernel(DiffProblem p)
                 D[a] = half_sum(sum[a]) * inv[a];
         }
     }
-    glam = half_sum(glam) * inv[1];
+    glam = kSumLambda ? half_sum(glam) * inv[1] : D[1];
     // What the dK, dV kernel needs of a row, also for those up to the end of the last tile
     // of 32.
     if (g == 0 && r < p.rows32) {
