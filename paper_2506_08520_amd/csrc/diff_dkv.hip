@@ -1,6 +1,9 @@
 // Backward pass of differential attention, second half: dK, dV and dlam, key by key, and
 // the calls of both halves (the formulas stand in diff_common.hpp).
+#include <algorithm>
 #include <type_traits>
+
+#include "nystra.h"
 
 #include "diff_common.hpp"
 
@@ -392,8 +395,30 @@ void plan_rows(DiffProblem *p, int waves)
     p->partial_row = 2 * p->d4 + p->dv4;
 }
 
-// The workspace's parts: a record of each row and its lambda, dlam's rows, and dK and dV by
-// row range.
+// Key ranges of the dQ kernel, for few rows over many keys: enough workgroups for the 256
+// CUs twice over, of at least four tiles each.  Only where the workgroups are half of the
+// CUs at most: 8 queries over 8192 keys, forward and backward, take 70 instead of 321 us
+// (fp32 153 instead of 1653 us), 8 heads of 2048 causal rows (128 workgroups) 185 instead of
+// 206 us, but 14 heads of 2048 rows (224) 315 instead of 297 us.  Up to 256 keys, where the
+// kernel walks over them twice, there are none.
+void plan_keys(DiffProblem *p, int waves)
+{
+    const int64_t rows = int64_t(p->R) * p->nq, units = int64_t(p->W) * p->G;
+    p->tiles = ceil_div(rows, 32 * waves);
+    p->dq_row = 2 * p->d4 + 4;
+    p->splits = 1;
+    p->chunk = p->nk;
+    const int64_t blocks = units * p->tiles;
+    if (p->nk <= NYSTRA_DIFF_SHORT_KEYS || blocks == 0 || blocks > 128)
+        return;
+    const int64_t most = ceil_div(p->nk, 128), want = (512 + blocks - 1) / blocks;
+    p->splits = int(want < most ? want : most);
+    p->chunk = ceil_div(ceil_div(p->nk, p->splits), 32) * 32;
+    p->splits = ceil_div(p->nk, p->chunk);
+}
+
+// The workspace's parts: a record of each row and its lambda, dlam's rows, and, one after the
+// other in the same place, dQ by key range and dK and dV by row range.
 struct Parts {
     int64_t stats, lambda, lam, partial;
 };
@@ -403,7 +428,8 @@ Parts parts_of(const DiffProblem &p)
     const int64_t units = int64_t(p.W) * p.G;
     return Parts{round256(units * p.rows32 * 16), round256(units * p.rows32 * 4),
                  round256(int64_t(p.W) * p.H * p.nq * 4),
-                 p.rsplits > 1 ? units * p.rsplits * p.nk * p.partial_row * 4 : 0};
+                 std::max(p.rsplits > 1 ? units * p.rsplits * p.nk * p.partial_row * 4 : 0,
+                          p.splits > 1 ? units * p.splits * p.R * p.nq * p.dq_row * 4 : 0)};
 }
 
 }  // namespace
@@ -412,6 +438,7 @@ size_t diff_backward_workspace(const DiffProblem &p)
 {
     DiffProblem t = p;
     plan_rows(&t, backward_waves(p.nk));
+    plan_keys(&t, backward_waves(int64_t(p.R) * p.nq));
     const Parts b = parts_of(t);
     return size_t(b.stats + b.lambda + b.lam + b.partial);
 }
@@ -429,15 +456,15 @@ hipError_t launch_diff_backward(DiffProblem p, void *workspace, hipStream_t s)
     p.vec_gv = store_vec(p.gv, p.dv, e);
     const int64_t rows = int64_t(p.R) * p.nq, units = int64_t(p.W) * p.G;
     const int wq = backward_waves(rows), wk = backward_waves(p.nk);
-    p.tiles = ceil_div(rows, 32 * wq);
     plan_rows(&p, wk);
+    plan_keys(&p, wq);
     const Parts b = parts_of(p);
     char *ws = static_cast<char *>(workspace);
     p.row_stats = reinterpret_cast<float4 *>(ws);
     p.row_lambda = reinterpret_cast<float *>(ws + b.stats);
     p.rows_lam = reinterpret_cast<float *>(ws + b.stats + b.lambda);
     p.partial = reinterpret_cast<float *>(ws + b.stats + b.lambda + b.lam);
-    hipError_t err = launch_diff_dq(p, wq, units * p.tiles, s);
+    hipError_t err = launch_diff_dq(p, wq, units * p.tiles * p.splits, s);
     if (err != hipSuccess)
         return err;
     const int64_t blocks = units * p.ktiles * p.rsplits;

@@ -47,7 +47,7 @@ diff_dq_kernel(DiffProblem p)
     __shared__ alignas(256) char lds[2 * Tiles::kBuffer];
     const uint32_t buf = lds_offset(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
-    const Place here = place(p, blockIdx.x, gridDim.x, p.tiles, 1, true);
+    const Place here = place(p, blockIdx.x, gridDim.x, p.tiles, p.splits, true);
     const int64_t unit = here.unit;
     const int w = int(here.unit / unsigned(p.G)), kvh = int(here.unit) - w * p.G;
     const int tile = here.tile;
@@ -58,13 +58,14 @@ diff_dq_kernel(DiffProblem p)
     const int len = window_len(p, w);
     const int limit = live ? key_limit(p, len, row.token) : 0;
     const int r1 = min(r0 + 32 * NW, nrows) - 1;
-    const int kend = tile_limit(p, len, r0, r1);
+    const int kbegin = here.split * p.chunk;
+    const int kend = min(tile_limit(p, len, r0, r1), kbegin + p.chunk);
     const float lam = p.lambda[row.head];
     const T *k0 = at<E>(p.k, w, 2 * kvh, 0), *v0 = at<E>(p.v, w, kvh, 0);
 
     Tiles tiles;
-    if (kend > 0)
-        tiles.fetch(p, k0, v0, 0, kend, buf);
+    if (kend > kbegin)
+        tiles.fetch(p, k0, v0, kbegin, kend, buf);
     Frag<E> q[2][DK / 16], go[DV / 16];
     float base[2], inv[2], D[2] = {0.f, 0.f};
 #pragma unroll
@@ -102,16 +103,16 @@ diff_dq_kernel(DiffProblem p)
     const float w1 = inv[0], w2 = -lam * inv[1];
     f16v acc[2][DK / 32] = {};
     float glam = 0.f;   // bf16 with kept maps; D_2 where that is as exact
-    if (kend > 0)
+    if (kend > kbegin)
         tiles.commit(buf);
     uint32_t t = buf, other = buf + Tiles::kBuffer;   // this tile's buffer and the next one's
     for (int sweep = KEPT ? 1 : 0; sweep < 2; ++sweep) {
         float sum[2] = {0.f, 0.f};
-        for (int key = 0; key < kend; key += KT) {
+        for (int key = kbegin; key < kend; key += KT) {
             Tiles::ready();
             const bool wrap = key + KT >= kend, more = !wrap || sweep == 0;
             if (more)
-                tiles.fetch(p, k0, v0, wrap ? 0 : key + KT, kend, other);
+                tiles.fetch(p, k0, v0, wrap ? kbegin : key + KT, kend, other);
             if (__any(key < limit)) {
                 const uint32_t krow = first_row<E, DK>(t), kcol = first_col<E, DK>(t);
                 const uint32_t vrow = first_row<E, DV>(t + Tiles::kV);
@@ -175,7 +176,7 @@ diff_dq_kernel(DiffProblem p)
     glam = kSumLambda ? half_sum(glam) * inv[1] : D[1];
     // What the dK, dV kernel needs of a row, also for those up to the end of the last tile
     // of 32.
-    if (g == 0 && r < p.rows32) {
+    if (g == 0 && here.split == 0 && r < p.rows32) {
         p.row_stats[unit * p.rows32 + r] =
             limit > 0 ? make_float4(base[0] - log2f(inv[0]), base[1] - log2f(inv[1]), D[0], D[1])
                       : make_float4(INFINITY, INFINITY, 0.f, 0.f);
@@ -183,6 +184,17 @@ diff_dq_kernel(DiffProblem p)
     }
     if (!live)
         return;
+    if (p.splits > 1) {
+        float *out = p.partial + ((unit * p.splits + here.split) * nrows + r) * p.dq_row;
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int i = 0; i < DK / 32; ++i)
+                store_block<F32>(out + a * p.d4, i, g, p.d4, true, acc[a][i]);
+        if (g == 0)
+            out[2 * p.d4] = kSumLambda || here.split == 0 ? glam : 0.f;
+        return;
+    }
     if (g == 0)
         p.rows_lam[unit * nrows + r] = glam;
     // A softmax over one key is constant: its gradient is zero, not the rounding of D.
@@ -193,6 +205,31 @@ diff_dq_kernel(DiffProblem p)
 #pragma unroll
         for (int i = 0; i < DK / 32; ++i)
             store_block<E>(dst, i, g, p.d, p.vec_gq, acc[a][i], scale);
+    }
+}
+
+// Adds up the key ranges of one row.
+template <class E>
+__global__ void __launch_bounds__(64) diff_dq_merge_kernel(DiffProblem p)
+{
+    const unsigned nrows = unsigned(p.R) * unsigned(p.nq);
+    const int64_t unit = blockIdx.x / nrows;
+    const int r = int(blockIdx.x - unit * nrows);
+    const int w = int(unsigned(unit) / unsigned(p.G)), kvh = int(unit) - w * p.G;
+    const Row row = row_of(p, kvh, r);
+    const float scale = key_limit(p, window_len(p, w), row.token) == 1 ? 0.f : p.scale;
+    const float *part = p.partial + (unit * p.splits * nrows + r) * p.dq_row;
+    const int64_t step = int64_t(nrows) * p.dq_row;
+    for (int col = threadIdx.x; col <= 2 * p.d4; col += 64) {
+        float s = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < p.splits; ++i)
+            s += part[i * step + col];
+        const int a = col >= p.d4, at_col = col - a * p.d4;
+        if (col == 2 * p.d4)
+            p.rows_lam[unit * nrows + r] = s;
+        else if (at_col < p.d)
+            E::store(at_out<E>(p.gq, w, 2 * row.head + a, row.token), at_col, scale * s);
     }
 }
 
@@ -232,6 +269,14 @@ void run_any(const DiffProblem &p, int waves, int64_t blocks, hipStream_t s)
 hipError_t launch_diff_dq(const DiffProblem &p, int waves, int64_t blocks, hipStream_t s)
 {
     p.dtype == 0 ? run_any<F32>(p, waves, blocks, s) : run_any<BF16>(p, waves, blocks, s);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess || p.splits == 1)
+        return err;
+    const dim3 rows(unsigned(int64_t(p.W) * p.G * p.R * p.nq));
+    if (p.dtype == 0)
+        diff_dq_merge_kernel<F32><<<rows, 64, 0, s>>>(p);
+    else
+        diff_dq_merge_kernel<BF16><<<rows, 64, 0, s>>>(p);
     return hipGetLastError();
 }
 

@@ -149,7 +149,7 @@ struct DiffProblem {
     uint32_t nq_mul;       // division by nq
     int nq_shift;
     bool even, store_o, vec_gq, vec_gk, vec_gv;
-    int tiles, ktiles, splits, chunk, rsplits, rchunk, d4, dv4, partial_row;
+    int tiles, ktiles, splits, chunk, rsplits, rchunk, d4, dv4, partial_row, dq_row;
     int64_t rows32;        // rows of a unit, up to a multiple of 32
     float *partial, *rows_lam, *row_lambda;   // [units][rows32] the last
     float4 *row_stats;     // [units][rows32]: L_1, L_2, D_1, D_2

@@ -67,6 +67,9 @@ SIZES = [
     (1, 1, 1, 300, 2, 64, 3, 0, None, False),
     (1, 6, 6, 1, 197, 30, 60, 2, None, False),
     (1, 3, 3, 40, 33, 64, 4, 1, None, False),        # more queries than keys
+    (4, 8, 2, 8, 1000, 64, 128, 2, [1000, 0, 1, 300], False),   # dQ by key ranges
+    (3, 4, 2, 5, 777, 33, 61, 2, [3, 777, 500], True),
+    (1, 2, 2, 300, 900, 21, 40, 1, None, False),
 ]
 
 
