@@ -18,7 +18,7 @@ diff_forward_kernel(DiffProblem p)
     using T = typename E::T;
     using Tiles = KeyTiles<E, DK, DV, 64 * NW, DIRECT>;
     constexpr int KT = Tiles::KT;
-    __shared__ alignas(256) char lds[2 * Tiles::kBuffer];
+    __shared__ alignas(256) char lds[Tiles::kBuffers * Tiles::kBuffer];
     const uint32_t buf = lds_offset(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
     const Place here = place(p, blockIdx.x, gridDim.x, p.tiles, p.splits, true);
@@ -53,7 +53,7 @@ diff_forward_kernel(DiffProblem p)
     if (kbegin < kend)
         tiles.commit(buf);
 
-    uint32_t t = buf, other = buf + Tiles::kBuffer;   // this tile's buffer and the next one's
+    uint32_t t = buf, other = buf + (Tiles::kBuffers - 1) * Tiles::kBuffer;   // this tile's buffer and the next one's
     for (int key = kbegin; key < kend; key += KT) {
         Tiles::ready();
         const bool more = key + KT < kend;
@@ -90,8 +90,10 @@ diff_forward_kernel(DiffProblem p)
                 }
             }
         }
-        if (more)
+        if (more) {
+            Tiles::vacate();
             tiles.commit(other);
+        }
         exchange(t, other);
     }
 #pragma unroll

@@ -616,7 +616,16 @@ __device__ inline Place place(const DiffProblem &p, unsigned b, unsigned n, unsi
     return Place{unit, int(tile), int(split)};
 }
 
-// Keys and values of a unit, tile after tile of KT keys, into two LDS buffers in turn:
+// Buffers of LDS for the tiles: two, or one where the next tile waits in registers and two
+// would leave SIMDs empty: workgroups of one wave, and of two in fp32, whose tile of three
+// terms takes up to 48 KB of a CU's 160.
+template <class E, int NT, bool DIRECT>
+constexpr int buffers()
+{
+    return !DIRECT && (NT == 64 || (E::bytes == 4 && NT == 128)) ? 1 : 2;
+}
+
+// Keys and values of a unit, tile after tile of KT keys, into the LDS buffers in turn:
 // fetch() starts on a tile, commit() ends it after the work on the one before, and ready()
 // is the barrier behind which it may be read.
 template <class E, int DK, int DV, int NT, bool DIRECT>
@@ -627,6 +636,7 @@ struct KeyTiles {
     using LV = Tile<E, DV>;
     // One buffer in LDS: the keys of both maps, then the values.
     static constexpr uint32_t kV = 2 * LK::kBytes, kBuffer = kV + LV::kBytes;
+    static constexpr int kBuffers = buffers<E, NT, DIRECT>();
     Stage<E, DK, 2 * KT, NT> k;   // both maps, one under the other
     Stage<E, DV, KT, NT> v;
 
@@ -663,6 +673,13 @@ struct KeyTiles {
         if constexpr (DIRECT)
             arrived();
         __syncthreads();
+    }
+
+    // Before commit(): where there is one buffer the work on it has to be done.
+    __device__ static inline void vacate()
+    {
+        if constexpr (kBuffers == 1)
+            __syncthreads();
     }
 };
 

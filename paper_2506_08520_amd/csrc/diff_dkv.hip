@@ -68,8 +68,9 @@ diff_dkv_kernel(DiffProblem p)
     constexpr uint32_t kMap = LQ::kBytes, kGo = 2 * kMap, kStat = kGo + LG::kBytes;
     constexpr uint32_t kLam = kStat + 16 * QT, kLim = kLam + 4 * QT;
     constexpr uint32_t kBuffer = (kLim + 4 * QT + 255) / 256 * 256;
-    __shared__ alignas(256) char lds[2 * kBuffer + (kLdsV ? NW * LG::kBytes : 0)];
-    const uint32_t buf = lds_offset(lds), vs = buf + 2 * kBuffer;
+    constexpr int kBuffers = buffers<E, NT, DIRECT>();
+    __shared__ alignas(256) char lds[kBuffers * kBuffer + (kLdsV ? NW * LG::kBytes : 0)];
+    const uint32_t buf = lds_offset(lds), vs = buf + kBuffers * kBuffer;
     if (int(blockIdx.x) < p.H) {
         sum_dlam<NT>(p, blockIdx.x, p.glam);
         return;
@@ -183,7 +184,7 @@ diff_dkv_kernel(DiffProblem p)
         fetch(r0, buf);
         commit(r0, buf);
     }
-    uint32_t t = buf, other = buf + kBuffer;   // this tile's buffer and the next one's
+    uint32_t t = buf, other = buf + (kBuffers - 1) * kBuffer;   // this tile's buffer and the next one's
     while (r0 < rend) {
         if constexpr (DIRECT)
             arrived();
@@ -270,8 +271,11 @@ diff_dkv_kernel(DiffProblem p)
                 }
             }
         }
-        if (r1 < rend)
+        if (r1 < rend) {
+            if (kBuffers == 1)
+                __syncthreads();
             commit(r1, other);
+        }
         exchange(t, other);
         r0 = r1;
     }

@@ -44,7 +44,7 @@ diff_dq_kernel(DiffProblem p)
     // fp32 takes the kept O_2: the matrix instruction's sums round towards one side, which
     // dO . V carries into every row alike (777 keys: 1.5e-6 from dO . V, 1.6e-7 so).
     constexpr bool kSumLambda = KEPT && E::bytes == 2;
-    __shared__ alignas(256) char lds[2 * Tiles::kBuffer];
+    __shared__ alignas(256) char lds[Tiles::kBuffers * Tiles::kBuffer];
     const uint32_t buf = lds_offset(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, c = lane & 31;
     const Place here = place(p, blockIdx.x, gridDim.x, p.tiles, p.splits, true);
@@ -105,7 +105,7 @@ diff_dq_kernel(DiffProblem p)
     float glam = 0.f;   // bf16 with kept maps; D_2 where that is as exact
     if (kend > kbegin)
         tiles.commit(buf);
-    uint32_t t = buf, other = buf + Tiles::kBuffer;   // this tile's buffer and the next one's
+    uint32_t t = buf, other = buf + (Tiles::kBuffers - 1) * Tiles::kBuffer;   // this tile's buffer and the next one's
     for (int sweep = KEPT ? 1 : 0; sweep < 2; ++sweep) {
         float sum[2] = {0.f, 0.f};
         for (int key = kbegin; key < kend; key += KT) {
@@ -163,8 +163,10 @@ diff_dq_kernel(DiffProblem p)
                         }
                 }
             }
-            if (more)
+            if (more) {
+                Tiles::vacate();
                 tiles.commit(other);
+            }
             exchange(t, other);
         }
         if (sweep == 0) {
