@@ -26,6 +26,8 @@
 // fp32 instructions of depth two, and within 2^-22 of it.
 #pragma once
 
+#include <type_traits>
+
 #include "device_common.hpp"
 #include "internal.hpp"
 
@@ -461,29 +463,38 @@ __device__ inline typename E::T *at_out(const DiffView &v, int64_t w, int64_t he
     return static_cast<typename E::T *>(v.data) + w * v.window + head * v.head + token * v.token;
 }
 
-template <class E>
+template <class E, bool ALIGNED>
 __device__ inline void store_vec4(typename E::T *at, f4 x)
 {
-    if constexpr (E::bytes == 4) {
-        *reinterpret_cast<f4 *>(at) = x;
-    } else {
-        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-        *reinterpret_cast<b4 *>(at) = __builtin_convertvector(x, b4);   // to nearest even
-    }
+    typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+    using V = std::conditional_t<E::bytes == 4, f4, b4>;
+    struct __attribute__((packed, aligned(E::bytes))) Any {
+        V v;
+    };
+    const V v = __builtin_convertvector(x, V);   // bf16: to nearest even
+    if constexpr (ALIGNED)
+        *reinterpret_cast<V *>(at) = v;
+    else
+        reinterpret_cast<Any *>(at)->v = v;
 }
 
 // Four consecutive elements of an output row from column `col`, those below `n`; `vec`
-// says that such groups are whole and aligned.
+// says that such groups are whole and aligned.  Others are stored whole at the elements'
+// alignment, and only a row's last one by elements.
 template <class E>
 __device__ inline void store4(typename E::T *row, int col, int n, bool vec, f4 x)
 {
     if (vec) {
         if (col < n)
-            store_vec4<E>(row + col, x);
+            store_vec4<E, true>(row + col, x);
+        return;
+    }
+    if (col + 4 <= n) {
+        store_vec4<E, false>(row + col, x);
         return;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 3; ++j)
         if (col + j < n) {
             if constexpr (E::bytes == 4)
                 row[col + j] = x[j];
@@ -507,7 +518,11 @@ __device__ inline void store_block(typename E::T *row, int i, int g, int n, bool
     if (vec && 32 * i + 32 <= n) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-            store_vec4<E>(row + 4 * g + 32 * i + 8 * t, v[t]);
+            store_vec4<E, true>(row + 4 * g + 32 * i + 8 * t, v[t]);
+    } else if (32 * i + 32 <= n) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            store_vec4<E, false>(row + 4 * g + 32 * i + 8 * t, v[t]);
     } else {
 #pragma unroll
         for (int t = 0; t < 4; ++t)

@@ -403,7 +403,9 @@ void plan_rows(DiffProblem *p, int waves)
 // CUs twice over, of at least four tiles each.  Only where the workgroups are half of the
 // CUs at most: 8 queries over 8192 keys, forward and backward, take 70 instead of 321 us
 // (fp32 153 instead of 1653 us), 8 heads of 2048 causal rows (128 workgroups) 185 instead of
-// 206 us, but 14 heads of 2048 rows (224) 315 instead of 297 us.  Up to 256 keys, where the
+// 206 us, but 14 heads of 2048 rows (224) 315 instead of 297 us; with one tile of rows to a
+// unit, whose sums are small, all of them (180 of 2 queries over 1457 keys, fp32: 78 instead
+// of 176 us for dQ, but 508 of 5 over 514 keys 188 instead of 168 us).  Up to 256 keys, where the
 // kernel walks over them twice, there are none.
 void plan_keys(DiffProblem *p, int waves)
 {
@@ -413,7 +415,7 @@ void plan_keys(DiffProblem *p, int waves)
     p->splits = 1;
     p->chunk = p->nk;
     const int64_t blocks = units * p->tiles;
-    if (p->nk <= NYSTRA_DIFF_SHORT_KEYS || blocks == 0 || blocks > 128)
+    if (p->nk <= NYSTRA_DIFF_SHORT_KEYS || blocks == 0 || blocks > (rows <= 32 ? 256 : 128))
         return;
     const int64_t most = ceil_div(p->nk, 128), want = (512 + blocks - 1) / blocks;
     p->splits = int(want < most ? want : most);
