@@ -369,17 +369,20 @@ int nystra_dropout(const void *X, const void *residual, void *Y, int64_t n, floa
  * Each is given as a nystra_view: its data and the strides of its first three dimensions.
  *
  * Keys.  kv_len (device int32 [n_windows], clamped to 0 .. n_k) gives every window a length
- * of its own; NULL: n_k.  Keys and values at or behind it are not read.  causal:
+ * of its own; NULL: n_k.  What keys and values hold at or behind it has no effect (the
+ * memory must be there).  causal:
  *   NYSTRA_CAUSAL_NONE   every query sees all keys below the length;
  *   NYSTRA_CAUSAL_START  query i sees keys 0 .. i (a batch padded at its end);
  *   NYSTRA_CAUSAL_END    query i sees keys 0 .. length - n_q + i: the queries are the
  *                        last n_q tokens of the sequence (new tokens over a cache).
- * A query that sees no key gets zeros, and passes no gradient.  Inside the length, keys and
- * values that a causal query does not see must be finite.
+ * A query that sees no key gets zeros, and passes no gradient; queries have no length of
+ * their own.  Inside the length, keys and values that a causal query does not see must be
+ * finite.
  *
- * Arithmetic.  Scores, softmax and accumulation are fp32.  fp32 runs on the fp32 matrix
- * cores; bf16 on the bf16 ones, with the probabilities (in the backward pass also the
- * gradients of the scores) rounded to bf16 for the products that take them.
+ * Arithmetic.  Scores, softmax and accumulation are fp32, the products run on the bf16
+ * matrix cores.  fp32 operands go there as three bf16 terms and six products, within 2^-22
+ * of the fp32 product (an infinity becomes NaN); for bf16 the probabilities (in the backward
+ * pass also the gradients of the scores) are rounded to bf16 for the products that take them.
  *
  * For training, sums (fp32 [n_windows][2 heads][n_q][2], 8-byte aligned: per row and map a
  * base b and the sum of 2^(s log2 e - b) over the visible scores s; 0 for a query without
