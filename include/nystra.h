@@ -386,11 +386,11 @@ int nystra_dropout(const void *X, const void *residual, void *Y, int64_t n, floa
  *
  * For training, sums (fp32 [n_windows][2 heads][n_q][2], 8-byte aligned: per row and map a
  * base b and the sum of 2^(s log2 e - b) over the visible scores s; 0 for a query without
- * keys) and, where n_k > NYSTRA_DIFF_SHORT_KEYS, maps
- * (fp32, 16-byte aligned: [n_windows][heads][n_q][d_v], the second map's output, for fp32;
- * [n_windows][heads][n_q][2][d_v], the second and the first map's, for bf16, whose O is
- * rounded) are stored for the backward pass; both are contiguous, and NULL for inference.
- * maps is NULL for shorter n_k.
+ * keys) and maps (fp32, 16-byte aligned) are stored for the backward pass; both are
+ * contiguous, and NULL for inference.  maps holds the second map's output for fp32,
+ * [n_windows][heads][n_q][d_v], and the second and the first map's for bf16, whose O is
+ * rounded, [n_windows][heads][n_q][2][d_v]; bf16 with n_k <= NYSTRA_DIFF_SHORT_KEYS keeps
+ * none (NULL).
  *
  * Backward: dQ, dK, dV in `dtype` (dK, dV summed over the heads that share them, zero at or
  * behind the length) and dlambda (fp32 [heads]) from dO and the same inputs, O, maps and sums.
@@ -409,7 +409,7 @@ typedef enum {
     NYSTRA_CAUSAL_END = 2
 } nystra_causal;
 
-#define NYSTRA_DIFF_SHORT_KEYS 256
+#define NYSTRA_DIFF_SHORT_KEYS 256   /* bf16: up to here no maps are kept */
 
 typedef struct nystra_view {
     void *data;

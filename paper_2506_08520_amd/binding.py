@@ -639,7 +639,7 @@ def nystra_diff_attn_forward(q, k, v, lam, scale=0.0, causal=CAUSAL_NONE, kv_len
     maps = sums = None
     if with_saved:
         sums = torch.empty((W, 2 * H, nq, 2), dtype=torch.float32, device=q.device)
-        if nk > DIFF_SHORT_KEYS:
+        if code != BF16 or nk > DIFF_SHORT_KEYS:
             # the second map's output, and in bf16, whose output is rounded, the first's
             maps = torch.empty((W, H, nq) + ((2, dv) if code == BF16 else (dv,)),
                                dtype=torch.float32, device=q.device)

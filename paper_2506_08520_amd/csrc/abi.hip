@@ -1108,8 +1108,7 @@ int nystra_diff_attn_forward(const nystra_view *Q, const nystra_view *K, const n
     if (misaligned(maps, 16) || misaligned(sums, 8) || misaligned(lambda, 4) ||
         misaligned(kv_len, 4))
         return NYSTRA_ERR_ALIGN;
-    // The backward pass reads the maps for many keys and forms their sums itself for few.
-    if ((maps && !sums) || (sums && (maps != nullptr) != (p.nk > NYSTRA_DIFF_SHORT_KEYS)))
+    if ((maps && !sums) || (sums && (maps != nullptr) != nystra::diff_keeps_maps(p)))
         return NYSTRA_ERR_NULL;
     const int64_t rows = int64_t(p.W) * p.H * p.nq;
     t[1] = Range{maps, rows * p.dv * (eb == 2 ? 8 : 4)};
@@ -1160,7 +1159,7 @@ int nystra_diff_attn_backward(const nystra_view *dO, const nystra_view *Q, const
             (rc = check_view(V, p.W, p.G, p.nk, p.dv, eb, false, &p.v, &t[7])) != NYSTRA_OK ||
             (rc = check_view(O, p.W, p.H, p.nq, p.dv, eb, false, &p.o, &t[8])) != NYSTRA_OK)
             return rc;
-        if (!lambda || !sums || (maps != nullptr) != (p.nk > NYSTRA_DIFF_SHORT_KEYS))
+        if (!lambda || !sums || (maps != nullptr) != nystra::diff_keeps_maps(p))
             return NYSTRA_ERR_NULL;
         if (misaligned(maps, 16) || misaligned(sums, 8) || misaligned(lambda, 4) ||
             misaligned(kv_len, 4))

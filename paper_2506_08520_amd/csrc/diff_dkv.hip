@@ -3,8 +3,6 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "nystra.h"
-
 #include "diff_common.hpp"
 
 namespace nystra {

@@ -25,13 +25,15 @@ __device__ inline float dot8(const Chunk<E> &a, const Chunk<F32> &b)
 
 // dQ, and per row D_1, D_2 and -dlam.  Rows as in the forward pass.  The exponentials are
 // the forward pass's, bit by bit, and their sums divide what is formed from them, so that
-// every row's probabilities add up to one and dlam, a sum of both signs, keeps its digits.  D_a comes from the
-// maps' outputs, D_2 = dO . O_2 and D_1 = dO . O_1 (fp32: dO . O + lam D_2), which the
-// forward pass keeps in fp32 (from outputs rounded to bf16, dQ was off by 0.0030 of its norm
-// at 4096 keys where rounding it alone costs 0.0017), or, where it kept none (up to 256 keys),
-// from a first walk over the keys: at 16 x 16 windows with heads of 32 / 64 that made the
-// forward pass 120 -> 79 us and this one 139 -> 146 us, by 400 MB less of traffic; at 512
-// keys the walk would cost more than it saves.
+// every row's probabilities add up to one and dlam, a sum of both signs, keeps its digits.
+//
+// D_a comes from the maps' outputs, D_2 = dO . O_2 and D_1 = dO . O_1 (fp32: dO . O +
+// lam D_2), which the forward pass keeps in fp32 (from outputs rounded to bf16, dQ was off
+// by 0.0030 of its norm at 4096 keys where rounding it alone costs 0.0017), or, where it kept
+// none (bf16 up to 256 keys), from a first walk over the keys: at 16 x 16 windows with heads
+// of 32 / 64 that made the forward pass 120 -> 79 us and this one 139 -> 146 us, by 400 MB
+// less of traffic; at 512 keys the walk would cost more than it saves, and fp32 with its six
+// products always.
 template <class E, int DK, int DV, int NW, bool DIRECT, bool KEPT>
 __global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>(!KEPT || E::bytes == 4)))
 diff_dq_kernel(DiffProblem p)
@@ -239,10 +241,13 @@ template <class E, int DK, int DV, int NW, bool DIRECT>
 void launch(const DiffProblem &p, int64_t blocks, hipStream_t s)
 {
     const dim3 grid(unsigned(blocks), 1, 1);
-    if (p.maps)
-        diff_dq_kernel<E, DK, DV, NW, DIRECT, true><<<grid, 64 * NW, 0, s>>>(p);
-    else
-        diff_dq_kernel<E, DK, DV, NW, DIRECT, false><<<grid, 64 * NW, 0, s>>>(p);
+    if constexpr (E::bytes == 2) {
+        if (!p.maps) {
+            diff_dq_kernel<E, DK, DV, NW, DIRECT, false><<<grid, 64 * NW, 0, s>>>(p);
+            return;
+        }
+    }
+    diff_dq_kernel<E, DK, DV, NW, DIRECT, true><<<grid, 64 * NW, 0, s>>>(p);
 }
 
 template <class E, int DK, int DV, int NW>

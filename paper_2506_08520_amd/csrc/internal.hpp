@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "nystra.h"
+
 namespace nystra {
 
 // Pooling grid of Step 1 (Sec. 2.2).  Token t = r * cols + c of the window
@@ -154,6 +156,12 @@ struct DiffProblem {
     float *partial, *rows_lam, *row_lambda;   // [units][rows32] the last
     float4 *row_stats;     // [units][rows32]: L_1, L_2, D_1, D_2
 };
+// Whether the forward pass keeps its maps' outputs for the backward pass, which forms what
+// it needs of them by a walk of its own for bf16 and few keys.
+inline bool diff_keeps_maps(const DiffProblem &p)
+{
+    return p.dtype == 0 || p.nk > NYSTRA_DIFF_SHORT_KEYS;
+}
 // Whether the grids of a call stay under the limits of a launch.
 bool diff_grid_fits(const DiffProblem &p);
 size_t diff_forward_workspace(const DiffProblem &p);

@@ -270,3 +270,12 @@ def test_graph_replays_equal_eager_calls(size):
         torch.cuda.synchronize()
         for a, b in zip(out, want):
             assert torch.equal(a, b), rep
+
+
+def test_no_windows():
+    """The gradient of lambda over no windows is zero, everything else is empty."""
+    q, k, v, lam, do = make(0, 4, 2, 8, 12, 16, 32, "f32")
+    o, saved = B.nystra_diff_attn_forward(q, k, v, lam, with_saved=True)
+    dq, dk, dv, dlam = B.nystra_diff_attn_backward(do, q, k, v, lam, o, saved)
+    assert o.shape == do.shape and dq.shape == q.shape and dk.shape == k.shape
+    assert (dlam == 0).all()

@@ -154,12 +154,14 @@ def test_diff_attention_tensors(L, call, outputs):
 
 
 def test_diff_attention_saved_values(L):
-    # many keys: both; few: the sums alone; inference: neither
+    # bf16, many keys: both; few: the sums alone; fp32: both; inference: neither
     assert forward(L, sums=None) == ENULL
     assert forward(L, maps=None) == ENULL
     assert forward(L, s=shape(nk=256)) == ENULL
     assert backward(L, maps=None) == ENULL and backward(L, sums=None) == ENULL
     assert backward(L, s=shape(nk=256)) == ENULL
+    assert forward(L, s=shape(nk=256), dtype=0, maps=None) == ENULL
+    assert backward(L, s=shape(nk=256), dtype=0, maps=None) == ENULL
     assert backward(L, dlam=None) == ENULL and backward(L, dlam=A[11] + 1) == EALIGN
     assert forward(L, sums=A[3]) == EOVERLAP and forward(L, maps=A[0]) == EOVERLAP
     assert backward(L, dlam=A[5]) == EOVERLAP and backward(L, dlam=A[8]) == EOVERLAP
