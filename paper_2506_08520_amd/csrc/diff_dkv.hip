@@ -1,5 +1,10 @@
 // Backward pass of differential attention, second half: dK, dV and dlam, key by key, and
 // the calls of both halves (the formulas stand in diff_common.hpp).
+//
+// Measured (sizes as in the forward pass): 4096 tokens 444 us, the matrix cores busy for
+// 32 % of the time (six products a tile, of which three meet operands by transposing
+// reads of LDS), 256 tokens 147 us, 19 %, of which 311 MB of traffic alone would take 62 us;
+// 777 tokens in fp32 145 us and 12 us for adding up the row ranges.
 #include <algorithm>
 #include <type_traits>
 
@@ -182,7 +187,8 @@ diff_dkv_kernel(DiffProblem p)
         fetch(r0, buf);
         commit(r0, buf);
     }
-    uint32_t t = buf, other = buf + (kBuffers - 1) * kBuffer;   // this tile's buffer and the next one's
+    // This tile's buffer and the next one's.
+    uint32_t t = buf, other = buf + (kBuffers - 1) * kBuffer;
     while (r0 < rend) {
         if constexpr (DIRECT)
             arrived();
