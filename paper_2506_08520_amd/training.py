@@ -22,7 +22,7 @@ from . import binding as B
 
 
 def _not_recorded(*tensors):
-    if torch.cuda.is_current_stream_capturing() and any(
+    if torch.is_grad_enabled() and torch.cuda.is_current_stream_capturing() and any(
             t is not None and t.requires_grad for t in tensors):
         raise RuntimeError("gradients in a recorded graph: call the binding's forward and "
                            "backward entry points instead")

@@ -156,6 +156,28 @@ def test_recorded_gradients_are_refused():
     assert torch.equal(y, T.dropout(T.layer_norm(frozen), 0.5, 3))
 
 
+def test_block_without_gradients_is_recorded():
+    """A block whose parameters ask for gradients, run under no_grad: every replay equals
+    the eager call on the inputs of its time."""
+    block = T.DifferentialTransformerBlock(32, 2, 8, shift=4, dtype=torch.bfloat16).eval()
+    x = torch.randn(1, 16, 24, 32, device="cuda", dtype=torch.bfloat16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.no_grad(), torch.cuda.stream(side):
+        block(x)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.no_grad(), torch.cuda.graph(graph):
+        y = block(x)
+    for _ in range(3):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        with torch.no_grad():
+            want = block(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+
+
 def test_arguments():
     for kw in (dict(dim=30, heads=4, window=8), dict(dim=32, heads=2, window=8, shift=8)):
         with pytest.raises(ValueError):
