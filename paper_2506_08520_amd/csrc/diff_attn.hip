@@ -20,7 +20,9 @@ using namespace diff;
 constexpr int kMerge = 256;       // threads of the merge kernel: one row
 constexpr int kFewSplits = 8;
 
-template <class E, int DK, int DV, int NW, bool DIRECT>
+// DIRECT: the bytes of the loads that bring keys and values to LDS (16 or 4), or 0 where
+// registers stage them.
+template <class E, int DK, int DV, int NW, int DIRECT>
 __global__ void __launch_bounds__(64 * NW, (NW == 1 && !DIRECT ? 1 : occupancy<E, DV>(NW == 2 && DV == 64)))
 diff_forward_kernel(DiffProblem p)
 {
@@ -54,7 +56,7 @@ diff_forward_kernel(DiffProblem p)
         const T *src = at<E>(p.q, w, 2 * row.head + a, row.token);
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
-            q[a][i] = as_frag(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
+            q[a][i] = as_frag(load_chunk<E, DIRECT == 16>(src + 16 * i + 8 * g,
                                                        p.d - 16 * i - 8 * g, live, p.d));
     }
     f16v acc[2][DV / 32] = {};
@@ -314,11 +316,18 @@ void run(const DiffProblem &p, const Plan &f, hipStream_t s)
     if constexpr (E::bytes == 2) {
         if (direct(p, p.q, p.d, 0) && direct(p, p.k, p.d, p.k.head + 32 * p.k.token) &&
             direct(p, p.v, p.dv, 32 * p.v.token)) {
-            diff_forward_kernel<E, DK, DV, NW, true><<<grid, 64 * NW, 0, s>>>(p);
+            diff_forward_kernel<E, DK, DV, NW, 16><<<grid, 64 * NW, 0, s>>>(p);
             return;
         }
+        if constexpr (DV == 64) {
+            if (direct(p, p.k, p.d, p.k.head + 32 * p.k.token, 4) &&
+                direct(p, p.v, p.dv, 32 * p.v.token, 4)) {
+                diff_forward_kernel<E, DK, DV, NW, 4><<<grid, 64 * NW, 0, s>>>(p);
+                return;
+            }
+        }
     }
-    diff_forward_kernel<E, DK, DV, NW, false><<<grid, 64 * NW, 0, s>>>(p);
+    diff_forward_kernel<E, DK, DV, NW, 0><<<grid, 64 * NW, 0, s>>>(p);
 }
 
 template <class E, int DK, int DV>

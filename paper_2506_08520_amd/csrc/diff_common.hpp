@@ -340,12 +340,18 @@ struct Stage {
     }
 };
 
-// 16 bytes from `base` plus each lane's offset to LDS, lane after lane from `lds` on, past
-// the registers.  Nothing waits for it but arrived().  base and lds are the wave's.
+// BYTES (16 or 4) from `base` plus each lane's offset to LDS, lane after lane from `lds` on,
+// past the registers.  Nothing waits for it but arrived().  base and lds are the wave's.
+template <int BYTES>
 __device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 :: "s"(lds), "v"(offset), "s"(base) : "memory");
+    static_assert(BYTES == 16 || BYTES == 4, "one of the instruction's widths");
+    if constexpr (BYTES == 16)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                     :: "s"(lds), "v"(offset), "s"(base) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                     :: "s"(lds), "v"(offset), "s"(base) : "memory");
 }
 
 __device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
@@ -360,23 +366,24 @@ __device__ inline unsigned thread_again()
     return thread;
 }
 
-// The same tile by loads that go to LDS directly, for rows of whole 16-byte chunks; at(row)
-// is the row's offset from `base` in elements, below 2^30.  Every lane loads: rows that are
+// The same tile by loads that go to LDS directly, for rows of whole and aligned groups of
+// BYTES; at(row) is the row's offset from `base` in elements, below 2^30.  Every lane loads: rows that are
 // not there must be given as another's (their products are masked), and columns from `cols`
-// on hold the last chunk again (the other operand is zero there).
-template <int COLS, int ROWS, int NT, class At>
+// on hold the last group again (the other operand is zero there).
+template <int COLS, int ROWS, int NT, int BYTES, class At>
 __device__ inline void direct_tile(uint32_t lds, const void *base, At at, int cols,
                                    unsigned thread = threadIdx.x)
 {
     using L = Tile<BF16, COLS>;
-    static_assert(ROWS * L::kRow % NT == 0, "whole waves");
-    const uint32_t to = lds + 1024 * __builtin_amdgcn_readfirstlane(thread / 64);
+    constexpr int kPer = 16 / BYTES, kRow = kPer * L::kRow, kWide = BYTES / 2;
+    static_assert(ROWS * kRow % NT == 0, "whole waves");
+    const uint32_t to = lds + 64 * BYTES * __builtin_amdgcn_readfirstlane(thread / 64);
 #pragma unroll
-    for (int i = 0; i < ROWS * L::kRow / NT; ++i) {
+    for (int i = 0; i < ROWS * kRow / NT; ++i) {
         const unsigned id = thread + i * NT;
-        const int row = id / L::kRow, chunk = int(id % L::kRow) ^ L::swap(row);
-        const int col = min(8 * chunk, cols - 8);
-        load_to_lds(base, 2 * uint32_t(at(row) + col), to + 16 * i * NT);
+        const int row = id / kRow, chunk = int(id % kRow / kPer) ^ L::swap(row);
+        const int col = min(8 * chunk + kWide * int(id % kPer), cols - kWide);
+        load_to_lds<BYTES>(base, 2 * uint32_t(at(row) + col), to + BYTES * i * NT);
     }
 }
 
@@ -634,7 +641,7 @@ __device__ inline Place place(const DiffProblem &p, unsigned b, unsigned n, unsi
 // Buffers of LDS for the tiles: two, or one where the next tile waits in registers and two
 // would leave SIMDs empty: workgroups of one wave, and of two in fp32, whose tile of three
 // terms takes up to 48 KB of a CU's 160.
-template <class E, int NT, bool DIRECT>
+template <class E, int NT, int DIRECT>
 constexpr int buffers()
 {
     return !DIRECT && (NT == 64 || (E::bytes == 4 && NT == 128)) ? 1 : 2;
@@ -643,7 +650,7 @@ constexpr int buffers()
 // Keys and values of a unit, tile after tile of KT keys, into the LDS buffers in turn:
 // fetch() starts on a tile, commit() ends it after the work on the one before, and ready()
 // is the barrier behind which it may be read.
-template <class E, int DK, int DV, int NT, bool DIRECT>
+template <class E, int DK, int DV, int NT, int DIRECT>
 struct KeyTiles {
     static constexpr int KT = 32;
     using T = typename E::T;
@@ -663,10 +670,11 @@ struct KeyTiles {
         v0 += key * p.v.token;
         if constexpr (DIRECT) {
             const int kh = int(p.k.head), kt = int(p.k.token), vt = int(p.v.token);
-            direct_tile<DK, 2 * KT, NT>(
+            direct_tile<DK, 2 * KT, NT, DIRECT>(
                 to, k0, [&](int row) { return (row / KT) * kh + min(row % KT, last) * kt; },
                 p.d);
-            direct_tile<DV, KT, NT>(to + kV, v0, [&](int row) { return min(row, last) * vt; }, p.dv);
+            direct_tile<DV, KT, NT, DIRECT>(to + kV, v0,
+                                            [&](int row) { return min(row, last) * vt; }, p.dv);
         } else {
             k.load([&](int row) { return k0 + (row / KT) * p.k.head + (row % KT) * p.k.token; },
                    [&](int row) { return row % KT <= last; }, p.d);
@@ -721,11 +729,12 @@ inline bool aligned(const DiffView &v, int width, int bytes, int to)
            (v.window | v.head | v.token | width) * bytes % to == 0;
 }
 
-// Whether tiles can be loaded to LDS directly: bf16 rows of whole 16-byte chunks, and
-// `span` elements, those of a tile or of a unit, within 32-bit offsets.
-inline bool direct(const DiffProblem &p, const DiffView &v, int width, int64_t span)
+// Whether tiles can be loaded to LDS directly: bf16 rows of whole and aligned groups of
+// `bytes`, and `span` elements, those of a tile or of a unit, within 32-bit offsets.
+inline bool direct(const DiffProblem &p, const DiffView &v, int width, int64_t span,
+                   int bytes = 16)
 {
-    return p.dtype == 1 && aligned(v, width, 2, 16) && span < (int64_t(1) << 30);
+    return p.dtype == 1 && aligned(v, width, 2, bytes) && span < (int64_t(1) << 30);
 }
 
 // Whether groups of four elements may be stored at once.

@@ -142,10 +142,10 @@ diff_dkv_kernel(DiffProblem p)
     };
     auto fetch = [&](int r0, uint32_t t) {
         if constexpr (DIRECT) {
-            direct_tile<DK, 2 * QT, NT>(
+            direct_tile<DK, 2 * QT, NT, 16>(
                 t, q0, [&](int i) { return q_row(r0 + i % QT, i / QT); }, p.d,
                 thread_again());
-            direct_tile<DV, QT, NT>(
+            direct_tile<DV, QT, NT, 16>(
                 t + kGo, go0, [&](int i) { return go_row(r0 + i); }, p.dv, thread_again());
         } else {
             sq.load([&](int i) { return q0 + q_row(r0 + i % QT, i / QT); },
@@ -157,9 +157,9 @@ diff_dkv_kernel(DiffProblem p)
         const float *lams = p.row_lambda + unit * p.rows32 + r0;
         if constexpr (DIRECT) {
             if (threadIdx.x < QT)
-                load_to_lds(stats, 16 * threadIdx.x, t + kStat);
+                load_to_lds<16>(stats, 16 * threadIdx.x, t + kStat);
             if (threadIdx.x < QT / 4)
-                load_to_lds(lams, 16 * threadIdx.x, t + kLam);
+                load_to_lds<16>(lams, 16 * threadIdx.x, t + kLam);
         } else if (threadIdx.x < QT) {
             sstat = *reinterpret_cast<const f4 *>(stats + threadIdx.x);
             slam = lams[threadIdx.x];

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>(!KEPT || E::bytes =
 diff_dq_kernel(DiffProblem p)
 {
     using T = typename E::T;
-    using Tiles = KeyTiles<E, DK, DV, 64 * NW, DIRECT>;
+    using Tiles = KeyTiles<E, DK, DV, 64 * NW, DIRECT ? 16 : 0>;
     constexpr int KT = Tiles::KT;
     // The row's part of -dlam is dO . O_2 = D_2.  bf16 forms it here from the probabilities,
     // where O_2 came from their roundings (323 keys: dlam off by 1.5e-3 from O_2, 4.8e-7 so).
