@@ -23,7 +23,7 @@ constexpr int kFewSplits = 8;
 // DIRECT: the bytes of the loads that bring keys and values to LDS (16 or 4), or 0 where
 // registers stage them.
 template <class E, int DK, int DV, int NW, int DIRECT>
-__global__ void __launch_bounds__(64 * NW, (NW == 1 && !DIRECT ? 1 : occupancy<E, DV>(NW == 2 && DV == 64)))
+__global__ void __launch_bounds__(64 * NW, (NW == 1 && !DIRECT ? 1 : NW == 2 && DIRECT == 4 ? 3 : occupancy<E, DV>(NW == 2 && DV == 64)))
 diff_forward_kernel(DiffProblem p)
 {
     using T = typename E::T;

@@ -56,7 +56,8 @@ __device__ inline float key_scale(const DiffProblem &p, int len)
 // that share the keys are summed in registers.  Keys at or behind the window's
 // length get zeros.  With few workgroups the rows are split over p.rsplits of them, whose
 // sums go to the workspace.  The first H workgroups add up dlam meanwhile.
-template <class E, int DK, int DV, int NW, bool DIRECT>
+// DIRECT as in the forward pass, for the queries and dO.
+template <class E, int DK, int DV, int NW, int DIRECT>
 __global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>(E::bytes == 4)))
 diff_dkv_kernel(DiffProblem p)
 {
@@ -94,7 +95,7 @@ diff_dkv_kernel(DiffProblem p)
         const T *src = at<E>(p.k, w, 2 * kvh + a, live ? key : 0);
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
-            k[a][i] = as_frag(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
+            k[a][i] = as_frag(load_chunk<E, DIRECT == 16>(src + 16 * i + 8 * g,
                                                        p.d - 16 * i - 8 * g, live, p.d));
     }
     if constexpr (kLdsV) {
@@ -105,14 +106,14 @@ diff_dkv_kernel(DiffProblem p)
             const int id = threadIdx.x + i * NT, row = id / LG::kRow, ch = id % LG::kRow;
             const bool in = kb + row < len;
             LG::store(vs + row / 32 * LG::kBytes, row % 32, ch,
-                      load_chunk<E, DIRECT>(v0 + (in ? kb + row : 0) * p.v.token + 8 * ch,
+                      load_chunk<E, DIRECT == 16>(v0 + (in ? kb + row : 0) * p.v.token + 8 * ch,
                                             p.dv - 8 * ch, in, p.dv));
         }
     } else {
         const T *src = at<E>(p.v, w, kvh, live ? key : 0);
 #pragma unroll
         for (int i = 0; i < DV / 16; ++i)
-            v[i] = as_frag(load_chunk<E, DIRECT>(src + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
+            v[i] = as_frag(load_chunk<E, DIRECT == 16>(src + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
                                                     live, p.dv));
     }
     f16v gk[2][DK / 32] = {}, gv[DV / 32] = {};
@@ -128,7 +129,7 @@ diff_dkv_kernel(DiffProblem p)
             from += QT;
         return from;
     };
-    using Off = std::conditional_t<DIRECT, int, int64_t>;
+    using Off = std::conditional_t<DIRECT != 0, int, int64_t>;
     // A row's place from the unit's first: the heads that share the keys lie behind each
     // other, head after head.
     const T *q0 = at<E>(p.q, w, 2 * kvh * p.R, 0), *go0 = at<E>(p.go, w, kvh * p.R, 0);
@@ -142,10 +143,10 @@ diff_dkv_kernel(DiffProblem p)
     };
     auto fetch = [&](int r0, uint32_t t) {
         if constexpr (DIRECT) {
-            direct_tile<DK, 2 * QT, NT, 16>(
+            direct_tile<DK, 2 * QT, NT, DIRECT>(
                 t, q0, [&](int i) { return q_row(r0 + i % QT, i / QT); }, p.d,
                 thread_again());
-            direct_tile<DV, QT, NT, 16>(
+            direct_tile<DV, QT, NT, DIRECT>(
                 t + kGo, go0, [&](int i) { return go_row(r0 + i); }, p.dv, thread_again());
         } else {
             sq.load([&](int i) { return q0 + q_row(r0 + i % QT, i / QT); },
@@ -364,11 +365,18 @@ void run(const DiffProblem &p, int64_t blocks, hipStream_t s)
         if (direct(p, p.k, p.d, 0) && direct(p, p.v, p.dv, 0) &&
             direct(p, p.q, p.d, 2 * p.R * p.q.head + p.nq * p.q.token) &&
             direct(p, p.go, p.dv, p.R * p.go.head + p.nq * p.go.token)) {
-            diff_dkv_kernel<E, DK, DV, NW, true><<<grid, 64 * NW, 0, s>>>(p);
+            diff_dkv_kernel<E, DK, DV, NW, 16><<<grid, 64 * NW, 0, s>>>(p);
             return;
         }
+        if constexpr (DV == 64) {
+            if (direct(p, p.q, p.d, 2 * p.R * p.q.head + p.nq * p.q.token, 4) &&
+                direct(p, p.go, p.dv, p.R * p.go.head + p.nq * p.go.token, 4)) {
+                diff_dkv_kernel<E, DK, DV, NW, 4><<<grid, 64 * NW, 0, s>>>(p);
+                return;
+            }
+        }
     }
-    diff_dkv_kernel<E, DK, DV, NW, false><<<grid, 64 * NW, 0, s>>>(p);
+    diff_dkv_kernel<E, DK, DV, NW, 0><<<grid, 64 * NW, 0, s>>>(p);
 }
 
 template <class E>

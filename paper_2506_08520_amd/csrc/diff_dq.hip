@@ -38,12 +38,13 @@ __device__ inline float dot8(const Chunk<E> &a, const Chunk<F32> &b)
 // of 32 / 64 that made the forward pass 120 -> 79 us and this one 139 -> 146 us, by 400 MB
 // less of traffic; at 512 keys the walk would cost more than it saves, and fp32 with its six
 // products always.
-template <class E, int DK, int DV, int NW, bool DIRECT, bool KEPT>
+// DIRECT as in the forward pass.
+template <class E, int DK, int DV, int NW, int DIRECT, bool KEPT>
 __global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>(!KEPT || E::bytes == 4)))
 diff_dq_kernel(DiffProblem p)
 {
     using T = typename E::T;
-    using Tiles = KeyTiles<E, DK, DV, 64 * NW, DIRECT ? 16 : 0>;
+    using Tiles = KeyTiles<E, DK, DV, 64 * NW, DIRECT>;
     constexpr int KT = Tiles::KT;
     // The row's part of -dlam is dO . O_2 = D_2.  bf16 forms it here from the probabilities,
     // where O_2 came from their roundings (323 keys: dlam off by 1.5e-3 from O_2, 4.8e-7 so).
@@ -79,7 +80,7 @@ diff_dq_kernel(DiffProblem p)
         const T *src = at<E>(p.q, w, 2 * row.head + a, row.token);
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
-            q[a][i] = as_frag(load_chunk<E, DIRECT>(src + 16 * i + 8 * g,
+            q[a][i] = as_frag(load_chunk<E, DIRECT == 16>(src + 16 * i + 8 * g,
                                                        p.d - 16 * i - 8 * g, live, p.d));
         const float2 sum = sum_row(p, w, row)[a * p.nq];
         base[a] = limit > 0 ? sum.x : INFINITY;   // exp2(-inf) = 0 where no key is seen
@@ -88,7 +89,7 @@ diff_dq_kernel(DiffProblem p)
     const T *gosrc = at<E>(p.go, w, row.head, row.token);
 #pragma unroll
     for (int i = 0; i < DV / 16; ++i)
-        go[i] = as_frag(load_chunk<E, DIRECT>(gosrc + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
+        go[i] = as_frag(load_chunk<E, DIRECT == 16>(gosrc + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
                                                  live, p.dv));
     if constexpr (KEPT) {
         const float *o2 = map_row<E>(p, w, row);
@@ -96,7 +97,7 @@ diff_dq_kernel(DiffProblem p)
 #pragma unroll 2   // more would hold more of the rows at once than there are registers
         for (int col = 8 * g; col < p.dv; col += 16) {
             const int n = p.dv - col;
-            const Chunk<E> x = load_chunk<E, DIRECT>(gosrc + col, n, live, p.dv);
+            const Chunk<E> x = load_chunk<E, DIRECT == 16>(gosrc + col, n, live, p.dv);
             D[0] += dot8(x, load_chunk<F32, false>(o1 + col, n, live, p.dv));
             D[1] += dot8(x, load_chunk<F32, false>(o2 + col, n, live, p.dv));
         }
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(64) diff_dq_merge_kernel(DiffProblem p)
     }
 }
 
-template <class E, int DK, int DV, int NW, bool DIRECT>
+template <class E, int DK, int DV, int NW, int DIRECT>
 void launch(const DiffProblem &p, int64_t blocks, hipStream_t s)
 {
     const dim3 grid(unsigned(blocks), 1, 1);
@@ -262,9 +263,13 @@ void run(const DiffProblem &p, int64_t blocks, hipStream_t s)
         if (direct(p, p.q, p.d, 0) && direct(p, p.go, p.dv, 0) &&
             direct(p, p.k, p.d, p.k.head + 32 * p.k.token) &&
             direct(p, p.v, p.dv, 32 * p.v.token))
-            return launch<E, DK, DV, NW, true>(p, blocks, s);
+            return launch<E, DK, DV, NW, 16>(p, blocks, s);
+        if constexpr (DV == 64)
+            if (direct(p, p.k, p.d, p.k.head + 32 * p.k.token, 4) &&
+                direct(p, p.v, p.dv, 32 * p.v.token, 4))
+                return launch<E, DK, DV, NW, 4>(p, blocks, s);
     }
-    launch<E, DK, DV, NW, false>(p, blocks, s);
+    launch<E, DK, DV, NW, 0>(p, blocks, s);
 }
 
 template <class E>
