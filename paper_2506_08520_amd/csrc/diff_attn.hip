@@ -23,7 +23,7 @@ constexpr int kFewSplits = 8;
 // DIRECT: the bytes of the loads that bring keys and values to LDS (16 or 4), or 0 where
 // registers stage them.
 template <class E, int DK, int DV, int NW, int DIRECT>
-__global__ void __launch_bounds__(64 * NW, (NW == 1 && !DIRECT ? 1 : NW == 2 && DIRECT == 4 ? 3 : occupancy<E, DV>(NW == 2 && DV == 64)))
+__global__ void __launch_bounds__(64 * NW, (NW == 1 && !DIRECT ? 1 : NW == 2 && DV == 64 && DIRECT == 4 ? 3 : occupancy<E, DV>(NW == 2 && DV == 64)))
 diff_forward_kernel(DiffProblem p)
 {
     using T = typename E::T;
@@ -319,12 +319,10 @@ void run(const DiffProblem &p, const Plan &f, hipStream_t s)
             diff_forward_kernel<E, DK, DV, NW, 16><<<grid, 64 * NW, 0, s>>>(p);
             return;
         }
-        if constexpr (DV == 64) {
-            if (direct(p, p.k, p.d, p.k.head + 32 * p.k.token, 4) &&
-                direct(p, p.v, p.dv, 32 * p.v.token, 4)) {
-                diff_forward_kernel<E, DK, DV, NW, 4><<<grid, 64 * NW, 0, s>>>(p);
-                return;
-            }
+        if (direct(p, p.k, p.d, p.k.head + 32 * p.k.token, 4) &&
+            direct(p, p.v, p.dv, 32 * p.v.token, 4)) {
+            diff_forward_kernel<E, DK, DV, NW, 4><<<grid, 64 * NW, 0, s>>>(p);
+            return;
         }
     }
     diff_forward_kernel<E, DK, DV, NW, 0><<<grid, 64 * NW, 0, s>>>(p);

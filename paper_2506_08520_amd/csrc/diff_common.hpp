@@ -731,6 +731,9 @@ inline bool aligned(const DiffView &v, int width, int bytes, int to)
 
 // Whether tiles can be loaded to LDS directly: bf16 rows of whole and aligned groups of
 // `bytes`, and `span` elements, those of a tile or of a unit, within 32-bit offsets.
+// 16 bytes where they fit; 4 otherwise, which still beat the way through registers: 256 x 6
+// windows of 256 tokens of 30 / 60, dQ 168 instead of 221 us, dK, dV 172 instead of 215 us;
+// 4 x 6 causal heads of 1024 tokens of 46 / 92, 57 instead of 103 us and 55 instead of 102 us.
 inline bool direct(const DiffProblem &p, const DiffView &v, int width, int64_t span,
                    int bytes = 16)
 {

@@ -368,12 +368,10 @@ void run(const DiffProblem &p, int64_t blocks, hipStream_t s)
             diff_dkv_kernel<E, DK, DV, NW, 16><<<grid, 64 * NW, 0, s>>>(p);
             return;
         }
-        if constexpr (DV == 64) {
-            if (direct(p, p.q, p.d, 2 * p.R * p.q.head + p.nq * p.q.token, 4) &&
-                direct(p, p.go, p.dv, p.R * p.go.head + p.nq * p.go.token, 4)) {
-                diff_dkv_kernel<E, DK, DV, NW, 4><<<grid, 64 * NW, 0, s>>>(p);
-                return;
-            }
+        if (direct(p, p.q, p.d, 2 * p.R * p.q.head + p.nq * p.q.token, 4) &&
+            direct(p, p.go, p.dv, p.R * p.go.head + p.nq * p.go.token, 4)) {
+            diff_dkv_kernel<E, DK, DV, NW, 4><<<grid, 64 * NW, 0, s>>>(p);
+            return;
         }
     }
     diff_dkv_kernel<E, DK, DV, NW, 0><<<grid, 64 * NW, 0, s>>>(p);

@@ -264,10 +264,9 @@ void run(const DiffProblem &p, int64_t blocks, hipStream_t s)
             direct(p, p.k, p.d, p.k.head + 32 * p.k.token) &&
             direct(p, p.v, p.dv, 32 * p.v.token))
             return launch<E, DK, DV, NW, 16>(p, blocks, s);
-        if constexpr (DV == 64)
-            if (direct(p, p.k, p.d, p.k.head + 32 * p.k.token, 4) &&
-                direct(p, p.v, p.dv, 32 * p.v.token, 4))
-                return launch<E, DK, DV, NW, 4>(p, blocks, s);
+        if (direct(p, p.k, p.d, p.k.head + 32 * p.k.token, 4) &&
+            direct(p, p.v, p.dv, 32 * p.v.token, 4))
+            return launch<E, DK, DV, NW, 4>(p, blocks, s);
     }
     launch<E, DK, DV, NW, 0>(p, blocks, s);
 }

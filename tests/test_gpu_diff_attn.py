@@ -70,6 +70,9 @@ SIZES = [
     (4, 8, 2, 8, 1000, 64, 128, 2, [1000, 0, 1, 300], False),   # dQ by key ranges
     (3, 4, 2, 5, 777, 33, 61, 2, [3, 777, 500], True),
     (1, 2, 2, 300, 900, 21, 40, 1, None, False),
+    (2, 8, 2, 1, 700, 46, 92, 2, [700, 33], False),      # rows of 4-byte groups, full width
+    (1, 2, 2, 70, 300, 46, 90, 0, None, True),
+    (2, 2, 1, 40, 50, 2, 2, 0, [50, 7], False),          # the narrowest of them
 ]
 
 
