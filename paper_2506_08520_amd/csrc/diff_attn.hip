@@ -5,9 +5,10 @@
 // instructions run beside the other's exponentials.  Keys are split over workgroups where
 // there are few rows.  Measured: 2 x 8 heads of 4096 tokens of 64 / 128 in bf16 251 us, the
 // matrix cores busy for 44 % of the time (the rest are exponentials and waits for LDS);
-// 256 x 6 of 256 tokens of 32 / 64 79 us, 26 %; 16 tokens of 16 heads over 4 x 8192 keys
-// at most 42 us, bound by memory (169 MB, 4.0 TB/s), and 5 us for the merge; 5 x 8 causal
-// heads of 777 tokens of 44 / 88 in fp32 110 and 13 us.
+// 256 x 6 of 256 tokens of 32 / 64 79 us, 26 %; 1024 x 6 of 64 tokens of 30 / 60 50 us,
+// bound by memory (203 MB, 4.1 TB/s) and by the latency of two tiles; 16 tokens of 16 heads
+// over 4 x 8192 keys at most 42 us, bound by memory (169 MB, 4.0 TB/s), and 5 us for the
+// merge; 5 x 8 causal heads of 777 tokens of 44 / 88 in fp32 110 and 13 us.
 #include <algorithm>
 
 #include "diff_common.hpp"
