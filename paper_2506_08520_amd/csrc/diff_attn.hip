@@ -299,11 +299,10 @@ Plan forward_plan(const DiffProblem &p)
     f.waves = waves_for(rows);
     f.tiles = ceil_div(rows, 32 * f.waves);
     const int64_t blocks = int64_t(p.W) * p.G * f.tiles;
-    const int64_t want = std::max<int64_t>(f.waves == 1 ? (2048 + blocks - 1) / blocks
-                                                        : (p.causal == 0 ? 1024 : 3072) / f.waves / blocks,
-                                               1);
+    const int64_t want = f.waves == 1 ? (2048 + blocks - 1) / blocks
+                                      : (p.causal == 0 ? 1 : 3) * 1024 / f.waves / blocks;
     const int64_t most = ceil_div(p.nk, 32 * f.waves);
-    f.splits = int(std::min(want, most));
+    f.splits = int(std::max<int64_t>(std::min(want, most), 1));
     f.chunk = ceil_div(ceil_div(p.nk, f.splits), 32) * 32;
     f.splits = ceil_div(p.nk, f.chunk);
     f.blocks = blocks * f.splits;

@@ -412,7 +412,7 @@ void plan_rows(DiffProblem *p, int waves)
 // Key ranges of the dQ kernel, for few rows over many keys: enough workgroups for the 256
 // CUs twice over, of at least four tiles each.  Only where the workgroups are half of the
 // CUs at most: 8 queries over 8192 keys, forward and backward, take 70 instead of 321 us
-// (fp32 153 instead of 1653 us), 8 heads of 2048 causal rows (128 workgroups) 185 instead of
+// (fp32, twice as many, 140 instead of 1653 us), 8 heads of 2048 causal rows (128 workgroups) 185 instead of
 // 206 us, but 14 heads of 2048 rows (224) 315 instead of 297 us; with one tile of rows to a
 // unit, whose sums are small, all of them (180 of 2 queries over 1457 keys, fp32: 78 instead
 // of 176 us for dQ, but 508 of 5 over 514 keys 188 instead of 168 us).  Up to 256 keys, where the
