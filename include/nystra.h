@@ -383,6 +383,8 @@ int nystra_dropout(const void *X, const void *residual, void *Y, int64_t n, floa
  * matrix cores.  fp32 operands go there as three bf16 terms and six products, within 2^-22
  * of the fp32 product (an infinity becomes NaN); for bf16 the probabilities (in the backward
  * pass also the gradients of the scores) are rounded to bf16 for the products that take them.
+ * A NaN among a query's scores makes its output NaN however the keys are divided; in fp32 one
+ * of the second map reaches the gradients of the first one, too (through O).
  *
  * For training, sums (fp32 [n_windows][2 heads][n_q][2], 8-byte aligned: per row and map a
  * base b and the sum of 2^(s log2 e - b) over the visible scores s; 0 for a query without

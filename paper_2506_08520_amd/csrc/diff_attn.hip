@@ -157,7 +157,9 @@ diff_forward_kernel(DiffProblem p)
     }
 }
 
-// Joins few key ranges, a thread to four columns of a row: each forms the weights itself.
+// Joins few key ranges, a thread to four columns of a row: each forms the weights itself.  A
+// range without a key has a sum of zero; one whose scores are all NaN has no maximum either,
+// but a sum of NaN, which has to reach the output.
 template <class E>
 __global__ void __launch_bounds__(kMerge)
 diff_merge_few_kernel(DiffProblem p, int64_t items)
@@ -189,7 +191,7 @@ diff_merge_few_kernel(DiffProblem p, int64_t items)
     for (int s = 0; s < kFewSplits; ++s)
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-            if (ml[s][2 * a] != -INFINITY) {
+            if (ml[s][2 * a + 1] != 0.f) {
                 const float e = fast_exp2(ml[s][2 * a] - m[a]);
                 l[a] = fmaf(e, ml[s][2 * a + 1], l[a]);
                 x[a] += e * *reinterpret_cast<const f4 *>(part + s * step + a * p.dv4 + col);
@@ -249,15 +251,13 @@ diff_merge_kernel(DiffProblem p)
 #pragma unroll
             for (int s = 0; s < kBatch; ++s)
                 mn = fmaxf(mn, mb[s]);
-            if (mn == -INFINITY)
-                continue;   // ranges without a key
-            const float alpha = fast_exp2(m - mn);
+            const float alpha = m == mn ? 1.f : fast_exp2(m - mn);
             l *= alpha;
             x *= alpha;
             m = mn;
 #pragma unroll
             for (int s = 0; s < kBatch; ++s) {
-                if (s0 + s < p.splits && mb[s] != -INFINITY) {
+                if (s0 + s < p.splits && lb[s] != 0.f) {   // as above
                     const float e = fast_exp2(mb[s] - m);
                     l = fmaf(e, lb[s], l);
                     x = fmaf(e, xb[s], x);

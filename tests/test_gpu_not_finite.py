@@ -1,0 +1,66 @@
+"""Differential attention with values that are not finite: NaN where the formulas have it
+and nowhere else, however the keys are divided over workgroups."""
+import pytest
+import torch
+
+from paper_2506_08520_amd import binding as B
+import operators_oracle as ref
+from test_gpu_diff_attn import lens, make
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+
+
+def call(q, k, v, lam, do, **kw):
+    o, saved = B.nystra_diff_attn_forward(q, k, v, lam, with_saved=True, **kw)
+    grads = B.nystra_diff_attn_backward(do, q, k, v, lam, o, saved, **kw)
+    only = B.nystra_diff_attn_forward(q, k, v, lam, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(only.isnan(), o.isnan())
+    return [t.cpu() for t in (o, *grads)]
+
+
+def same_nan(got, want, name, more=False):
+    bad = want.isnan() & ~got.isnan() if more else got.isnan() != want.isnan()
+    assert not bad.any(), f"{name}: {int(bad.sum())} of {bad.numel()}, first {bad.nonzero()[0]}"
+
+
+def compare(ts, clean, got, what, more=()):
+    """NaN in the elements where the formulas in 64 bits have it (of the results in `more`
+    also in others); what is finite is that of the same inputs without NaN, within the bounds
+    of that call."""
+    q, k, v, lam, do = (t.cpu() for t in ts)
+    want = ref.diff_attention(q, k, v, lam, do=do)
+    bounds = ref.diff_attention(*(t.cpu() for t in clean[:4]), do=clean[4].cpu())
+    for x, (y, _), (z, e), name in zip(got, want, bounds, ("O", "dQ", "dK", "dV", "dlam")):
+        same_nan(x, y, f"{what} {name}", name in more)
+        ok = ~y.isnan() & ~x.isnan()
+        assert ((x.double() - z).abs() <= e)[ok].all(), f"{what} {name}"
+
+
+# One workgroup to a row's keys; up to eight key ranges; more than eight.
+SPLITS = [(3, 4, 2, 70, 90), (2, 4, 2, 3, 200), (2, 4, 2, 1, 1000)]
+
+
+@pytest.mark.parametrize("dtype,d,dv", [("f32", 30, 60), ("bf16", 30, 60), ("bf16", 32, 64),
+                                        ("bf16", 31, 61), ("bf16", 64, 128), ("f32", 44, 88)])
+@pytest.mark.parametrize("W,H,G,nq,nk", SPLITS)
+@pytest.mark.parametrize("where", ["query", "query2", "key", "keys", "value"])
+def test_nan(W, H, G, nq, nk, dtype, d, dv, where):
+    clean = make(W, H, G, nq, nk, d, dv, dtype)
+    q, k, v, lam, do = (t.clone() for t in clean)
+    if where == "query":       # first map of head 1
+        q[1, 2, nq // 2, d - 1] = NAN
+    elif where == "query2":    # second map of head 2
+        q[0, 5, nq - 1, 0] = NAN
+    elif where == "key":
+        k[1, 0, nk // 2, 3] = NAN
+    elif where == "keys":      # one key range and more of them
+        k[0, 3, 32:64] = NAN
+    else:
+        v[1, 1, nk - 1, dv - 1] = NAN
+    ts = (q, k, v, lam, do)
+    # fp32 forms D_1 from O, into which the second map's NaN went
+    more = ("dQ", "dK") if dtype == "f32" and where in ("query2", "keys") else ()
+    compare(ts, clean, call(*ts), f"{where} {dtype} {nq}x{nk}", more)
