@@ -255,9 +255,11 @@ diff_dkv_kernel(DiffProblem p)
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const bool one = *lds_at<int>(t + kLim + 4 * reg_row(i, g)) == 1;   // as in the dQ kernel
-                    s[0][i] = one ? 0.f : s[0][i];
-                    s[1][i] = one ? 0.f : s[1][i];
+                    // A factor, as in the dQ kernel: NaN stays.
+                    const float keep =
+                        *lds_at<int>(t + kLim + 4 * reg_row(i, g)) == 1 ? 0.f : 1.f;
+                    s[0][i] *= keep;
+                    s[1][i] *= keep;
                 }
             }
             part();

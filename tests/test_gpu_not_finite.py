@@ -64,3 +64,16 @@ def test_nan(W, H, G, nq, nk, dtype, d, dv, where):
     # fp32 forms D_1 from O, into which the second map's NaN went
     more = ("dQ", "dK") if dtype == "f32" and where in ("query2", "keys") else ()
     compare(ts, clean, call(*ts), f"{where} {dtype} {nq}x{nk}", more)
+
+
+@pytest.mark.parametrize("dtype,d,dv", [("f32", 30, 60), ("bf16", 30, 60), ("bf16", 31, 61)])
+@pytest.mark.parametrize("nq", [70, 300])
+def test_nan_of_a_row_with_one_key(nq, dtype, d, dv):
+    """A softmax over one NaN score is NaN, and so is the gradient of its key."""
+    q, k, v, lam, do = make(2, 1, 1, nq, nq, d, dv, dtype)
+    q[1, 0, 0, 5] = NAN
+    o, dq, dk, dv_, dlam = call(q, k, v, lam, do, causal=B.CAUSAL_START)
+    assert o[1, 0, 0].isnan().all() and not o[1, 0, 1:].isnan().any()
+    assert dq[1, 0, 0].isnan().all() and not dq[1, 0, 1:].isnan().any()
+    assert dk[1, 0, 0].isnan().all() and dv_[1, 0, 0].isnan().all()
+    assert not any(t[0].isnan().any() for t in (o, dq, dk, dv_))
