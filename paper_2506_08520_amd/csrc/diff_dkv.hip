@@ -131,14 +131,20 @@ diff_dkv_kernel(DiffProblem p)
     };
     using Off = std::conditional_t<DIRECT != 0, int, int64_t>;
     // A row's place from the unit's first: the heads that share the keys lie behind each
-    // other, head after head.
+    // other, head after head.  The first row of a head that sees a key stands for those in
+    // front of it, whose probabilities are zero.
     const T *q0 = at<E>(p.q, w, 2 * kvh * p.R, 0), *go0 = at<E>(p.go, w, kvh * p.R, 0);
-    auto q_row = [&](int r, int a) {
+    const int first = p.causal == 2 && len > 0 ? max(0, p.nq - len) : 0;
+    auto place_of = [&](int r) {
         const Row row = row_of(p, 0, min(r, nrows - 1));
+        return Row{row.head, max(row.token, first)};
+    };
+    auto q_row = [&](int r, int a) {
+        const Row row = place_of(r);
         return (2 * row.head + a) * Off(p.q.head) + row.token * Off(p.q.token);
     };
     auto go_row = [&](int r) {
-        const Row row = row_of(p, 0, min(r, nrows - 1));
+        const Row row = place_of(r);
         return row.head * Off(p.go.head) + row.token * Off(p.go.token);
     };
     auto fetch = [&](int r0, uint32_t t) {

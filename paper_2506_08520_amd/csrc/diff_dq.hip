@@ -64,6 +64,8 @@ diff_dq_kernel(DiffProblem p)
     const Row row = row_of(p, kvh, live ? r : r0);
     const int len = window_len(p, w);
     const int limit = live ? key_limit(p, len, row.token) : 0;
+    // What a row without keys holds has no effect: it counts as zeros.
+    const bool seeing = limit > 0;
     const int r1 = min(r0 + 32 * NW, nrows) - 1;
     const int kbegin = here.split * p.chunk;
     const int kend = min(tile_limit(p, len, r0, r1), kbegin + p.chunk);
@@ -81,25 +83,25 @@ diff_dq_kernel(DiffProblem p)
 #pragma unroll
         for (int i = 0; i < DK / 16; ++i)
             q[a][i] = as_frag(load_chunk<E, DIRECT == 16>(src + 16 * i + 8 * g,
-                                                       p.d - 16 * i - 8 * g, live, p.d));
+                                                       p.d - 16 * i - 8 * g, seeing, p.d));
         const float2 sum = sum_row(p, w, row)[a * p.nq];
-        base[a] = limit > 0 ? sum.x : INFINITY;   // exp2(-inf) = 0 where no key is seen
-        inv[a] = limit > 0 && sum.y != 0.f ? 1.f / sum.y : 0.f;
+        base[a] = seeing ? sum.x : INFINITY;   // exp2(-inf) = 0 where no key is seen
+        inv[a] = seeing && sum.y != 0.f ? 1.f / sum.y : 0.f;
     }
     const T *gosrc = at<E>(p.go, w, row.head, row.token);
 #pragma unroll
     for (int i = 0; i < DV / 16; ++i)
         go[i] = as_frag(load_chunk<E, DIRECT == 16>(gosrc + 16 * i + 8 * g, p.dv - 16 * i - 8 * g,
-                                                 live, p.dv));
+                                                 seeing, p.dv));
     if constexpr (KEPT) {
         const float *o2 = map_row<E>(p, w, row);
         const float *o1 = E::bytes == 2 ? o2 + p.dv : at<F32>(p.o, w, row.head, row.token);
 #pragma unroll 2   // more would hold more of the rows at once than there are registers
         for (int col = 8 * g; col < p.dv; col += 16) {
             const int n = p.dv - col;
-            const Chunk<E> x = load_chunk<E, DIRECT == 16>(gosrc + col, n, live, p.dv);
-            D[0] += dot8(x, load_chunk<F32, false>(o1 + col, n, live, p.dv));
-            D[1] += dot8(x, load_chunk<F32, false>(o2 + col, n, live, p.dv));
+            const Chunk<E> x = load_chunk<E, DIRECT == 16>(gosrc + col, n, seeing, p.dv);
+            D[0] += dot8(x, load_chunk<F32, false>(o1 + col, n, seeing, p.dv));
+            D[1] += dot8(x, load_chunk<F32, false>(o2 + col, n, seeing, p.dv));
         }
         if (E::bytes == 4)
             D[0] = fmaf(lam, D[1], D[0]);
@@ -188,8 +190,8 @@ diff_dq_kernel(DiffProblem p)
     // of 32.
     if (g == 0 && here.split == 0 && r < p.rows32) {
         p.row_stats[unit * p.rows32 + r] =
-            limit > 0 ? make_float4(base[0] - log2f(inv[0]), base[1] - log2f(inv[1]), D[0], D[1])
-                      : make_float4(INFINITY, INFINITY, 0.f, 0.f);
+            seeing ? make_float4(base[0] - log2f(inv[0]), base[1] - log2f(inv[1]), D[0], D[1])
+                   : make_float4(INFINITY, INFINITY, 0.f, 0.f);
         p.row_lambda[unit * p.rows32 + r] = lam;
     }
     if (!live)

@@ -77,3 +77,24 @@ def test_nan_of_a_row_with_one_key(nq, dtype, d, dv):
     assert dq[1, 0, 0].isnan().all() and not dq[1, 0, 1:].isnan().any()
     assert dk[1, 0, 0].isnan().all() and dv_[1, 0, 0].isnan().all()
     assert not any(t[0].isnan().any() for t in (o, dq, dk, dv_))
+
+
+@pytest.mark.parametrize("dtype,d,dv", [("f32", 30, 60), ("bf16", 30, 60), ("bf16", 32, 64),
+                                        ("bf16", 31, 61), ("bf16", 64, 128)])
+@pytest.mark.parametrize("nq,nk,kv_len", [(40, 40, [25, 40, 0]), (70, 300, [1, 300, 69]),
+                                          (9, 600, [8, 0, 3])])
+def test_queries_without_keys_pass_no_gradient(nq, nk, kv_len, dtype, d, dv):
+    """Rows in front of a sequence that is shorter than the queries: whatever they and their
+    gradients hold, the results are those of zeros there."""
+    kw = dict(causal=B.CAUSAL_END, kv_len=lens(kv_len))
+    q, k, v, lam, do = make(3, 4, 2, nq, nk, d, dv, dtype)
+    q2, do2 = q.clone(), do.clone()
+    for w, n in enumerate(kv_len):
+        unseen = max(0, nq - n)
+        q[w, :, :unseen], do[w, :, :unseen] = 0, 0
+        q2[w, :, :unseen:2], q2[w, :, 1:unseen:2] = NAN, float("inf")
+        do2[w, :, :unseen] = NAN
+    want, got = call(q, k, v, lam, do, **kw), call(q2, k, v, lam, do2, **kw)
+    for x, y, name in zip(got, want, ("O", "dQ", "dK", "dV", "dlam")):
+        assert torch.equal(x, y), name
+        assert torch.isfinite(y).all(), name
