@@ -131,8 +131,8 @@ diff_dkv_kernel(DiffProblem p)
     };
     using Off = std::conditional_t<DIRECT != 0, int, int64_t>;
     // A row's place from the unit's first: the heads that share the keys lie behind each
-    // other, head after head.  The first row of a head that sees a key stands for those in
-    // front of it, whose probabilities are zero.
+    // other, head after head.  The last row stands for those behind it, whose probabilities
+    // are zero, and the first one that sees a key for those of its head in front of it.
     const T *q0 = at<E>(p.q, w, 2 * kvh * p.R, 0), *go0 = at<E>(p.go, w, kvh * p.R, 0);
     const int first = p.causal == 2 && len > 0 ? max(0, p.nq - len) : 0;
     auto place_of = [&](int r) {
@@ -156,9 +156,9 @@ diff_dkv_kernel(DiffProblem p)
                 t + kGo, go0, [&](int i) { return go_row(r0 + i); }, p.dv, thread_again());
         } else {
             sq.load([&](int i) { return q0 + q_row(r0 + i % QT, i / QT); },
-                    [&](int i) { return r0 + i % QT < nrows; }, p.d);
+                    [](int) { return true; }, p.d);
             sgo.load([&](int i) { return go0 + go_row(r0 + i); },
-                     [&](int i) { return r0 + i < nrows; }, p.dv);
+                     [](int) { return true; }, p.dv);
         }
         const float4 *stats = p.row_stats + unit * p.rows32 + r0;
         const float *lams = p.row_lambda + unit * p.rows32 + r0;

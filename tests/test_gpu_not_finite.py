@@ -98,3 +98,28 @@ def test_queries_without_keys_pass_no_gradient(nq, nk, kv_len, dtype, d, dv):
     for x, y, name in zip(got, want, ("O", "dQ", "dK", "dV", "dlam")):
         assert torch.equal(x, y), name
         assert torch.isfinite(y).all(), name
+
+
+@pytest.mark.parametrize("d,dv", [(31, 61), (64, 128)])
+@pytest.mark.parametrize("nq,nk", [(70, 90), (3, 200), (40, 300)])
+def test_minus_infinity_scores_in_bf16(nq, nk, d, dv):
+    """A key of -inf against positive queries has the probability zero at any width; only the
+    gradient of the queries meets it again, as 0 x inf in its column."""
+    q, k, v, lam, do = make(2, 2, 1, nq, nk, d, dv, "bf16")
+    q[..., d - 1] = q[..., d - 1].abs() + 0.5
+    k[1, 0, nk // 3, d - 1] = -float("inf")
+    k[1, 1, nk // 3, d - 1] = -float("inf")
+    k[1, 1, nk - 1, d - 1] = -float("inf")
+    o, dq, dk, dv_, dlam = call(q, k, v, lam, do)
+    cpu = [t.cpu() for t in (q, k, v, lam, do)]
+    want = ref.diff_attention(*cpu[:4], do=cpu[4])
+    same_nan(dq, want[1][0], "dQ")
+    finite = dq[..., :d - 1]
+    assert torch.isfinite(finite).all()
+    # The bounds are those of the call with zeros for the infinities.  A probability of zero
+    # has no error; the others grow by 1 / (1 - P) of at most two keys' shares, below 2 where
+    # P < 1/2: the scores are within a few units and the keys 90 at least.
+    cpu[1] = torch.where(cpu[1].isinf(), 0, cpu[1])
+    bound = ref.diff_attention(*cpu[:4], do=cpu[4])
+    assert ((o.double() - want[0][0]).abs() <= 2 * bound[0][1]).all()
+    assert torch.isfinite(dk).all() and torch.isfinite(dv_).all() and torch.isfinite(dlam).all()
