@@ -341,17 +341,19 @@ struct Stage {
 };
 
 // BYTES (16 or 4) from `base` plus each lane's offset to LDS, lane after lane from `lds` on,
-// past the registers.  Nothing waits for it but arrived().  base and lds are the wave's.
+// past the registers.  Nothing waits for it but arrived().  base and lds are the wave's; lds
+// is the compiler's to put into m0, which the instruction reads one wait state later at the
+// earliest.
 template <int BYTES>
 __device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t lds)
 {
     static_assert(BYTES == 16 || BYTES == 4, "one of the instruction's widths");
     if constexpr (BYTES == 16)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                     :: "s"(lds), "v"(offset), "s"(base) : "memory");
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                     :: "v"(offset), "s"(base), "{m0}"(lds) : "memory");
     else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-                     :: "s"(lds), "v"(offset), "s"(base) : "memory");
+        asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1"
+                     :: "v"(offset), "s"(base), "{m0}"(lds) : "memory");
 }
 
 __device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
