@@ -341,19 +341,24 @@ struct Stage {
 };
 
 // BYTES (16 or 4) from `base` plus each lane's offset to LDS, lane after lane from `lds` on,
-// past the registers.  Nothing waits for it but arrived().  base and lds are the wave's; lds
-// is the compiler's to put into m0, which the instruction reads one wait state later at the
-// earliest.
+// past the registers.  Nothing waits for it but arrived().  base and lds are the wave's.
+// A vector memory instruction may read an SGPR that a VALU instruction wrote (a base from
+// v_readfirstlane, or one that was kept in a vector register) five wait states later at the
+// earliest, and m0 one after its writing; the compiler does not look into the statement for
+// either.  Scalar instructions wait by themselves, and so do reads of what they wrote: base
+// is copied by one, which is m0's wait state, too.
 template <int BYTES>
 __device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t lds)
 {
     static_assert(BYTES == 16 || BYTES == 4, "one of the instruction's widths");
+    uint32_t m0;
+    const void *from;
     if constexpr (BYTES == 16)
-        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                     :: "v"(offset), "s"(base), "{m0}"(lds) : "memory");
+        asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 %1, %4\n\tglobal_load_lds_dwordx4 %3, %1"
+                     : "=&{m0}"(m0), "=&s"(from) : "s"(lds), "v"(offset), "s"(base) : "memory");
     else
-        asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1"
-                     :: "v"(offset), "s"(base), "{m0}"(lds) : "memory");
+        asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 %1, %4\n\tglobal_load_lds_dword %3, %1"
+                     : "=&{m0}"(m0), "=&s"(from) : "s"(lds), "v"(offset), "s"(base) : "memory");
 }
 
 __device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
