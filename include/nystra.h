@@ -375,14 +375,17 @@ int nystra_dropout(const void *X, const void *residual, void *Y, int64_t n, floa
  *   NYSTRA_CAUSAL_START  query i sees keys 0 .. i (a batch padded at its end);
  *   NYSTRA_CAUSAL_END    query i sees keys 0 .. length - n_q + i: the queries are the
  *                        last n_q tokens of the sequence (new tokens over a cache).
- * A query that sees no key gets zeros, and passes no gradient; queries have no length of
- * their own.  Inside the length, keys and values that a causal query does not see must be
- * finite.
+ * A query that sees no key gets zeros, and passes no gradient whatever it holds; queries have
+ * no length of their own.  Inside the length, keys and values that a causal query does not
+ * see must be finite, and for the backward pass so must the queries and dO that a key is not
+ * seen by: they meet probabilities of zero in products.
  *
  * Arithmetic.  Scores, softmax and accumulation are fp32, the products run on the bf16
  * matrix cores.  fp32 operands go there as three bf16 terms and six products, within 2^-22
  * of the fp32 product (an infinity becomes NaN); for bf16 the probabilities (in the backward
  * pass also the gradients of the scores) are rounded to bf16 for the products that take them.
+ * In either type an infinity in an operand may give NaN where the formulas have a finite
+ * value: bf16 rows may be filled up with copies of their last elements, times zero.
  * A NaN among a query's scores makes its output NaN however the keys are divided; in fp32 one
  * of the second map reaches the gradients of the first one, too (through O).
  *
