@@ -134,8 +134,10 @@ def dropout(x, p, seed, offset=0, residual=None):
 
 
 def differential_attention(q, k, v, lam, scale=0.0, causal=B.CAUSAL_NONE, kv_len=None):
-    """binding.nystra_diff_attn_forward, differentiable in q, k, v and lam."""
+    """binding.nystra_diff_attn_forward, differentiable in q, k, v and lam (of any type: it
+    counts in fp32)."""
     _not_recorded(q, k, v, lam)
+    lam = lam.float()
     return _DiffAttention.apply(q, k, v, lam, scale, causal, kv_len)
 
 
@@ -168,12 +170,13 @@ class DifferentialWindowAttention(nn.Module):
         self.qkv = nn.Linear(dim, 3 * dim, **kw)
         self.proj = nn.Linear(dim, dim, **kw)
         self.norm = LayerNorm(dim // heads, **kw)
-        # fp32 whatever the layer's type: lam is the difference of two exponentials.
+        # fp32 whatever the layer's type, and formed in fp32 also where the module was moved to
+        # another one: lam is the difference of two exponentials.
         self.lam = nn.Parameter(0.1 * torch.randn(4, heads, dim // (2 * heads), device=device))
 
     def weights(self):
         """lam, fp32 [heads]."""
-        a1, b1, a2, b2 = self.lam
+        a1, b1, a2, b2 = self.lam.float()
         return torch.exp((a1 * b1).sum(-1)) - torch.exp((a2 * b2).sum(-1)) + self.lam_init
 
     def forward(self, x):
