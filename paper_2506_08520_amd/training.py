@@ -120,17 +120,23 @@ class _PackedDiffAttention(torch.autograd.Function):
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
-    """LayerNorm over the last dimension, differentiable in x, weight and bias."""
+    """LayerNorm over the last dimension, differentiable in x, weight and bias.  Weights of
+    another type are rounded to x's, half a step of it relative to each, as a layer of that
+    type holds them; their gradients come in their own."""
     _not_recorded(x, weight, bias)
+    weight, bias = (None if t is None else t.to(x.dtype) for t in (weight, bias))
     return _LayerNorm.apply(x, weight, bias, eps)
 
 
 def dropout(x, p, seed, offset=0, residual=None):
     """residual + dropout(x), differentiable in both; the mask is a function of seed and
-    offset and is formed again in the backward pass."""
+    offset and is formed again in the backward pass.  Of two types the sum is of the wider
+    one: a bf16 branch leaves an fp32 residual stream in fp32."""
     _not_recorded(x, residual)
-    return _Dropout.apply(x.contiguous(), None if residual is None else residual.contiguous(),
-                          p, seed, offset)
+    if residual is not None:
+        dtype = torch.promote_types(x.dtype, residual.dtype)
+        x, residual = x.to(dtype), residual.to(dtype).contiguous()
+    return _Dropout.apply(x.contiguous(), residual, p, seed, offset)
 
 
 def differential_attention(q, k, v, lam, scale=0.0, causal=B.CAUSAL_NONE, kv_len=None):

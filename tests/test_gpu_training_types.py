@@ -51,3 +51,50 @@ def test_attention_takes_lam_in_any_type():
         outs.append((o, t.grad))
     assert torch.equal(outs[0][0], outs[1][0])
     assert outs[0][1].dtype == BF and torch.equal(outs[0][1], outs[1][1].to(BF))
+
+
+def test_layer_norm_takes_parameters_of_another_type():
+    """fp32 weights of bf16 rows count as bf16 ones; their gradients come in fp32."""
+    x, dy = randn(37, 60, dtype=BF), randn(37, 60, dtype=BF, seed=1)
+    w, b = randn(60, seed=2) + 1, randn(60, seed=3)
+    got, want = [], []
+    for out, dt in ((got, torch.float32), (want, BF)):
+        xx, ww, bb = (t.clone().requires_grad_() for t in (x, w.to(dt), b.to(dt)))
+        y = T.layer_norm(xx, ww, bb)
+        y.backward(dy)
+        out += [y.detach(), xx.grad, ww.grad, bb.grad]
+    assert got[2].dtype == got[3].dtype == torch.float32 and got[0].dtype == BF
+    for a, c in zip(got, want):
+        assert torch.equal(a, c.to(a.dtype))
+
+
+@pytest.mark.parametrize("branch,stream", [(BF, torch.float32), (torch.float32, BF)])
+def test_dropout_onto_a_residual_of_another_type(branch, stream):
+    """The sum is of the wider type, as torch's is."""
+    x, r, dy = randn(5, 77, dtype=branch), randn(5, 77, dtype=stream, seed=1), randn(5, 77, seed=2)
+    xx, rr = x.clone().requires_grad_(), r.clone().requires_grad_()
+    y = T.dropout(xx, 0.3, 11, 2, residual=rr)
+    y.backward(dy)
+    assert y.dtype == torch.float32
+    assert torch.equal(y, B.nystra_dropout(x.float(), 0.3, 11, 2, residual=r.float()))
+    assert torch.equal(xx.grad, B.nystra_dropout(dy, 0.3, 11, 2).to(branch))
+    assert torch.equal(rr.grad, dy.to(stream))
+
+
+def test_block_under_autocast():
+    """Linear layers in bf16 beside fp32 parameters: the residual stream and every gradient
+    stay in fp32, and the output is the fp32 block's to within bf16's steps."""
+    block = make_block()
+    x, dy = randn(2, 16, 16, 60), randn(2, 16, 16, 60, seed=1)
+    ref = block(x, seed=5)
+    xx = x.clone().requires_grad_()
+    with torch.autocast("cuda", dtype=BF):
+        y = block(xx, seed=5)
+    y.backward(dy)
+    assert y.dtype == torch.float32
+    # Each branch passes about ten tensors rounded to bf16 (2^-8 each at most) on its way; the
+    # head norm's gain of a row's error is its mean size over its deviation, a few units.
+    assert (y - ref).norm() <= 40 * 2.0 ** -8 * (ref - x).norm()
+    for name, t in [("x", xx), *block.named_parameters()]:
+        assert t.grad is not None and t.grad.dtype == torch.float32, name
+        assert torch.isfinite(t.grad).all(), name
