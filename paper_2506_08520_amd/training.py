@@ -119,11 +119,22 @@ class _PackedDiffAttention(torch.autograd.Function):
         return grad, dlam, None
 
 
+def _row_strided(x):
+    """Whether x [..., C] is a list of rows at one stride, none of them over another."""
+    try:
+        return B._rows(x, x.shape[-1]) >= x.shape[-1]
+    except (IndexError, ValueError):
+        return False
+
+
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
     """LayerNorm over the last dimension, differentiable in x, weight and bias.  Weights of
     another type are rounded to x's, half a step of it relative to each, as a layer of that
-    type holds them; their gradients come in their own."""
+    type holds them; their gradients come in their own.  Rows that do not lie at one stride
+    are copied."""
     _not_recorded(x, weight, bias)
+    if not _row_strided(x):
+        x = x.contiguous()
     weight, bias = (None if t is None else t.to(x.dtype) for t in (weight, bias))
     return _LayerNorm.apply(x, weight, bias, eps)
 

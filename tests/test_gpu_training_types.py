@@ -98,3 +98,19 @@ def test_block_under_autocast():
     for name, t in [("x", xx), *block.named_parameters()]:
         assert t.grad is not None and t.grad.dtype == torch.float32, name
         assert torch.isfinite(t.grad).all(), name
+
+
+@pytest.mark.parametrize("layout", ["permuted", "cut", "broadcast", "columns"])
+def test_layer_norm_of_any_layout(layout):
+    """Rows that do not lie at one stride are copied, as torch's own layer does."""
+    base = randn(4, 6, 5, 32)
+    x = {"permuted": lambda: base.permute(2, 0, 1, 3), "cut": lambda: base[:, :4, 1:4],
+         "broadcast": lambda: base[:1, :1].expand(3, 2, 5, 32),
+         "columns": lambda: base.transpose(-1, -2)}[layout]()
+    norm = T.LayerNorm(x.shape[-1], device="cuda")
+    dy = randn(*x.shape, seed=4)
+    xx, cc = x.detach().requires_grad_(), x.contiguous().requires_grad_()
+    y, z = norm(xx), norm(cc)
+    assert torch.equal(y, z)
+    (gx,), (gc,) = torch.autograd.grad(y, xx, dy), torch.autograd.grad(z, cc, dy)
+    assert torch.equal(gx, gc)
