@@ -21,9 +21,13 @@ from torch.autograd.function import once_differentiable
 from . import binding as B
 
 
+def _differentiated(*tensors):
+    """Whether a backward pass may follow: without one nothing is kept for it."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 def _not_recorded(*tensors):
-    if torch.is_grad_enabled() and torch.cuda.is_current_stream_capturing() and any(
-            t is not None and t.requires_grad for t in tensors):
+    if _differentiated(*tensors) and torch.cuda.is_current_stream_capturing():
         raise RuntimeError("gradients in a recorded graph: call the binding's forward and "
                            "backward entry points instead")
 
@@ -36,7 +40,9 @@ def _not_recorded_backward():
 
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, eps):
+    def forward(ctx, x, weight, bias, eps, keep):
+        if not keep:
+            return B.nystra_layer_norm_forward(x, weight, bias, eps)
         y, mean, rstd = B.nystra_layer_norm_forward(x, weight, bias, eps, with_stats=True)
         ctx.save_for_backward(x, weight, mean, rstd)
         return y
@@ -48,7 +54,7 @@ class _LayerNorm(torch.autograd.Function):
         x, weight, mean, rstd = ctx.saved_tensors
         dx, dw, db = B.nystra_layer_norm_backward(dy.contiguous(), x, weight, mean, rstd)
         need = ctx.needs_input_grad
-        return dx, dw if need[1] else None, db if need[2] else None, None
+        return dx, dw if need[1] else None, db if need[2] else None, None, None
 
 
 class _Dropout(torch.autograd.Function):
@@ -68,9 +74,12 @@ class _Dropout(torch.autograd.Function):
 
 class _DiffAttention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, lam, scale, causal, kv_len):
-        o, saved = B.nystra_diff_attn_forward(q, k, v, lam, scale=scale, causal=causal,
-                                              kv_len=kv_len, with_saved=True)
+    def forward(ctx, q, k, v, lam, scale, causal, kv_len, keep):
+        o = B.nystra_diff_attn_forward(q, k, v, lam, scale=scale, causal=causal, kv_len=kv_len,
+                                       with_saved=keep)
+        if not keep:
+            return o
+        o, saved = o
         ctx.save_for_backward(q, k, v, lam, o, kv_len, *saved)
         ctx.args = dict(scale=scale, causal=causal)
         return o
@@ -82,7 +91,7 @@ class _DiffAttention(torch.autograd.Function):
         q, k, v, lam, o, kv_len, maps, sums = ctx.saved_tensors
         grads = B.nystra_diff_attn_backward(do.contiguous(), q, k, v, lam, o, (maps, sums),
                                             kv_len=kv_len, **ctx.args)
-        return (*grads, None, None, None)
+        return (*grads, None, None, None, None)
 
 
 def _packed_views(qkv, heads):
@@ -98,12 +107,13 @@ class _PackedDiffAttention(torch.autograd.Function):
     """On the projection's output, whose gradient is written as one tensor."""
 
     @staticmethod
-    def forward(ctx, qkv, lam, heads):
+    def forward(ctx, qkv, lam, heads, keep):
         W, N, C3 = qkv.shape
         out = qkv.new_empty(W, N, heads, C3 // 3 // heads)
-        _, saved = B.nystra_diff_attn_forward(*_packed_views(qkv, heads), lam, with_saved=True,
-                                              out=out.transpose(1, 2))
-        ctx.save_for_backward(qkv, lam, out, *saved)
+        got = B.nystra_diff_attn_forward(*_packed_views(qkv, heads), lam, with_saved=keep,
+                                         out=out.transpose(1, 2))
+        if keep:
+            ctx.save_for_backward(qkv, lam, out, *got[1])
         return out
 
     @staticmethod
@@ -116,7 +126,7 @@ class _PackedDiffAttention(torch.autograd.Function):
         *_, dlam = B.nystra_diff_attn_backward(
             do.contiguous().transpose(1, 2), *_packed_views(qkv, heads), lam,
             out.transpose(1, 2), (maps, sums), grads=_packed_views(grad, heads))
-        return grad, dlam, None
+        return grad, dlam, None, None
 
 
 def _row_strided(x):
@@ -136,7 +146,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     if not _row_strided(x):
         x = x.contiguous()
     weight, bias = (None if t is None else t.to(x.dtype) for t in (weight, bias))
-    return _LayerNorm.apply(x, weight, bias, eps)
+    return _LayerNorm.apply(x, weight, bias, eps, _differentiated(x, weight, bias))
 
 
 def dropout(x, p, seed, offset=0, residual=None):
@@ -155,7 +165,8 @@ def differential_attention(q, k, v, lam, scale=0.0, causal=B.CAUSAL_NONE, kv_len
     counts in fp32)."""
     _not_recorded(q, k, v, lam)
     lam = lam.float()
-    return _DiffAttention.apply(q, k, v, lam, scale, causal, kv_len)
+    return _DiffAttention.apply(q, k, v, lam, scale, causal, kv_len,
+                                _differentiated(q, k, v, lam))
 
 
 class LayerNorm(nn.LayerNorm):
@@ -206,7 +217,8 @@ class DifferentialWindowAttention(nn.Module):
         win = x.view(Bn, H // w, w, W // w, w, C).transpose(2, 3).reshape(-1, w * w, C)
         qkv, lam = self.qkv(win), self.weights()
         _not_recorded(qkv, lam)
-        o = _PackedDiffAttention.apply(qkv, lam, self.heads)      # [windows, N, heads, C / heads]
+        # [windows, N, heads, C / heads]
+        o = _PackedDiffAttention.apply(qkv, lam, self.heads, _differentiated(qkv, lam))
         o = self.norm(o) * (1.0 - self.lam_init)
         y = self.proj(o.flatten(2))
         y = y.view(Bn, H // w, W // w, w, w, C).transpose(2, 3).reshape(Bn, H, W, C)

@@ -114,3 +114,43 @@ def test_layer_norm_of_any_layout(layout):
     assert torch.equal(y, z)
     (gx,), (gc,) = torch.autograd.grad(y, xx, dy), torch.autograd.grad(z, cc, dy)
     assert torch.equal(gx, gc)
+
+
+def test_nothing_is_kept_without_gradients(monkeypatch):
+    """Statistics, sums and maps are for a backward pass only."""
+    kept = []
+
+    def watch(name, arg):
+        f = getattr(B, name)
+
+        def call(*a, **kw):
+            kept.append(bool(kw.get(arg)))
+            return f(*a, **kw)
+        monkeypatch.setattr(B, name, call)
+    watch("nystra_layer_norm_forward", "with_stats")
+    watch("nystra_diff_attn_forward", "with_saved")
+    block = make_block()
+    x = randn(1, 16, 16, 60)
+    want = block(x, seed=5)
+    assert kept == [True] * 4
+    del kept[:]
+    with torch.no_grad():
+        assert torch.equal(block(x, seed=5), want)
+    block.requires_grad_(False)
+    assert torch.equal(block(x, seed=5), want)
+    q, k, v = (randn(2, h, 20, w, dtype=BF, seed=h) for h, w in ((4, 16), (4, 16), (2, 32)))
+    T.differential_attention(q, k, v, torch.tensor([0.3, 0.7], device="cuda"))
+    assert kept == [False] * 9
+    T.differential_attention(q.requires_grad_(), k, v, torch.tensor([0.3, 0.7], device="cuda"))
+    assert kept[9:] == [True]
+
+
+def test_forward_mode_is_refused():
+    """A tangent is not dropped in silence where no backward pass follows."""
+    import torch.autograd.forward_ad as fwd
+    with fwd.dual_level():
+        x = fwd.make_dual(randn(4, 32), randn(4, 32, seed=1))
+        with pytest.raises(RuntimeError):
+            T.layer_norm(x)
+        with pytest.raises(RuntimeError):
+            T.dropout(x, 0.5, 1)
