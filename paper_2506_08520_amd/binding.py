@@ -34,6 +34,8 @@ STATIC_SCRATCH_BYTES = 32 << 20   # NYSTRA_STATIC_SCRATCH_BYTES
 BLOCK_NYSTROM, BLOCK_EXACT = 0, 1
 CAUSAL_NONE, CAUSAL_START, CAUSAL_END = 0, 1, 2
 DIFF_SHORT_KEYS = 256             # NYSTRA_DIFF_SHORT_KEYS
+NORM_MAX_CHANNELS = 4096
+DIFF_MAX_WIDTH = 64               # of queries and keys; of values twice that
 
 
 class NystraError(RuntimeError):

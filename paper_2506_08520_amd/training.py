@@ -174,6 +174,9 @@ class LayerNorm(nn.LayerNorm):
 
     def __init__(self, channels, eps=1e-5, **kw):
         super().__init__(channels, eps=eps, **kw)
+        if (len(self.normalized_shape) != 1 or
+                not 1 <= self.normalized_shape[0] <= B.NORM_MAX_CHANNELS):
+            raise ValueError(f"expected one dimension of 1 to {B.NORM_MAX_CHANNELS} channels")
 
     def forward(self, x):
         return layer_norm(x, self.weight, self.bias, self.eps)
@@ -190,6 +193,8 @@ class DifferentialWindowAttention(nn.Module):
         super().__init__()
         if dim % (2 * heads) != 0:
             raise ValueError("2 heads must divide dim")
+        if dim // (2 * heads) > B.DIFF_MAX_WIDTH:
+            raise ValueError(f"heads of more than {B.DIFF_MAX_WIDTH} channels to a map")
         if not 0 <= shift < window:
             raise ValueError("shift must be in [0, window)")
         kw = dict(dtype=dtype, device=device)
