@@ -21,10 +21,30 @@ using namespace diff;
 constexpr int kMerge = 256;       // threads of the merge kernel: one row
 constexpr int kFewSplits = 8;
 
+// Waves to a SIMD that the kernel is compiled for.
+// Narrow workgroups of two waves (up to 64 rows, the windows' form) whose tiles need no
+// registers on their way: three, since all of them wait for the same two tiles.  Those with
+// 16-byte loads fit by themselves; those with 4-byte loads keep five registers in memory for
+// it: 1024 x 6 windows of 64 tokens of 14 / 28 take 34 instead of 41 us at two waves, of 22 / 44
+// 45 instead of 50, of 30 / 60 54 instead of 56, of 49 tokens of 30 / 60 49 instead of 54.
+// Single waves that stage their tiles in registers: one, for the token form (16 x 16 heads over
+// 4 x 2048 keys of 31 / 62 in fp32 44 instead of 52 us at two; 6144 windows of 32 tokens of
+// 31 / 61 in fp32 99 instead of 91, of 63 / 127 in bf16 126 instead of 111, of 16 tokens 77
+// instead of 91).
+template <class E, int DV, int NW, int DIRECT>
+constexpr int forward_occupancy()
+{
+    if (NW == 1 && !DIRECT)
+        return 1;
+    if (NW == 2 && DV == 64)
+        return DIRECT ? 3 : occupancy<E, DV>(true);
+    return occupancy<E, DV>(false);
+}
+
 // DIRECT: the bytes of the loads that bring keys and values to LDS (16 or 4), or 0 where
 // registers stage them.
 template <class E, int DK, int DV, int NW, int DIRECT>
-__global__ void __launch_bounds__(64 * NW, (NW == 1 && !DIRECT ? 1 : NW == 2 && DV == 64 && DIRECT == 4 ? 3 : occupancy<E, DV>(NW == 2 && DV == 64)))
+__global__ void __launch_bounds__(64 * NW, (forward_occupancy<E, DV, NW, DIRECT>()))
 diff_forward_kernel(DiffProblem p)
 {
     using T = typename E::T;

@@ -37,7 +37,10 @@ __device__ inline float dot8(const Chunk<E> &a, const Chunk<F32> &b)
 // none (bf16 up to 256 keys), from a first walk over the keys: at 16 x 16 windows with heads
 // of 32 / 64 that made the forward pass 120 -> 79 us and this one 139 -> 146 us, by 400 MB
 // less of traffic; at 512 keys the walk would cost more than it saves, and fp32 with its six
-// products always.
+// products always.  Forward and backward pass of 393216 rows with the walk and without:
+// 64 keys of 32 / 64 193 and 302 us, of 64 / 128 (where the walk leaves one wave to a SIMD)
+// 439 and 647; 128 keys 228 and 315, 507 and 628; 256 keys 313 and 360, 674 and 697; but of
+// 44 / 88, which 4-byte loads bring, 524 and 596 at 128 keys, 734 and 695 at 256.
 // DIRECT as in the forward pass.
 template <class E, int DK, int DV, int NW, int DIRECT, bool KEPT>
 __global__ void __launch_bounds__(64 * NW, (occupancy<E, DV>(!KEPT || E::bytes == 4)))
