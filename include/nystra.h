@@ -311,7 +311,8 @@ int nystra_select_variant(int N, int d_h, int m, int dtype, const nystra_opts *o
 /* ---- Training and serving a layer: LayerNorm, dropout, differential attention ----
  * The conventions at the top hold here too (streams, errors, no allocation, kernel
  * launches only), except that tensors may be strided where strides are given, in
- * elements and not negative; the innermost dimension is always contiguous.  Sums,
+ * elements and not negative (at most 2^40, and 2^46 over a dimension); the innermost
+ * dimension is always contiguous.  Sums,
  * softmax statistics and normalisation are fp32.  No result depends on the order
  * in which workgroups run: the same call gives the same bits. */
 

@@ -824,7 +824,13 @@ int check_norm(int64_t rows, int channels, int dtype)
 
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
-bool bad_stride(int64_t stride, int64_t least) { return stride < least || stride > kMaxStride; }
+// Elements that a tensor spans at most: more than any memory holds, and its bytes fit 64 bits.
+constexpr int64_t kMaxSpan = int64_t(1) << 46;
+
+bool bad_stride(int64_t stride, int64_t least, int64_t rows)
+{
+    return stride < least || stride > kMaxStride || (rows - 1) > kMaxSpan / stride;
+}
 
 int64_t rows_range(int64_t rows, int64_t stride, int channels, int eb)
 {
@@ -876,7 +882,8 @@ int check_view(const nystra_view *v, int64_t windows, int64_t heads, int64_t tok
     for (int i = 0; i < 3; ++i) {
         if (size[i] == 1)
             stride[i] = 0;   // never stepped over, whatever the caller holds there
-        if (stride[i] < 0 || stride[i] > kMaxStride)
+        if (stride[i] < 0 || stride[i] > kMaxStride ||
+            (stride[i] > 0 && size[i] - 1 > kMaxSpan / stride[i]))
             return NYSTRA_ERR_SHAPE;
         last += (size[i] - 1) * stride[i];
     }
@@ -933,7 +940,7 @@ int nystra_layer_norm_forward(const void *X, int64_t x_stride, const void *weigh
         return NYSTRA_OK;
     if (!X || !Y || !mean != !rstd)
         return NYSTRA_ERR_NULL;
-    if (bad_stride(x_stride, channels) || bad_stride(y_stride, channels))
+    if (bad_stride(x_stride, channels, rows) || bad_stride(y_stride, channels, rows))
         return NYSTRA_ERR_SHAPE;
     const int eb = dtype_bytes(dtype);
     if (misaligned(X, eb) || misaligned(Y, eb) || misaligned(weight, eb) || misaligned(bias, eb) ||
@@ -990,8 +997,9 @@ int nystra_layer_norm_backward(const void *dY, int64_t dy_stride, const void *X,
         return rc;
     if (rows > 0 && (!dY || !X || !mean || !rstd || !dX))
         return NYSTRA_ERR_NULL;
-    if (rows > 0 && (bad_stride(dy_stride, channels) || bad_stride(x_stride, channels) ||
-                     bad_stride(dx_stride, channels)))
+    if (rows > 0 &&
+        (bad_stride(dy_stride, channels, rows) || bad_stride(x_stride, channels, rows) ||
+         bad_stride(dx_stride, channels, rows)))
         return NYSTRA_ERR_SHAPE;
     const int eb = dtype_bytes(dtype);
     for (const void *t : {dY, X, weight, static_cast<const void *>(dX),
