@@ -1,8 +1,8 @@
 // Forward pass of differential attention (the formulas stand in diff_common.hpp).
 //
 // One walk over the keys with the running maximum and sum of both maps, whose outputs stay
-// apart in registers (each has its own maximum).  Two waves to a SIMD: one's matrix
-// instructions run beside the other's exponentials.  Keys are split over workgroups where
+// apart in registers (each has its own maximum).  Two or three waves to a SIMD (fp32 at full
+// width: one): one's matrix instructions run beside the other's exponentials.  Keys are split over workgroups where
 // there are few rows.  Measured: 2 x 8 heads of 4096 tokens of 64 / 128 in bf16 251 us, the
 // matrix cores busy for 44 % of the time (the rest are exponentials and waits for LDS);
 // 256 x 6 of 256 tokens of 32 / 64 79 us, 26 %; 1024 x 6 of 64 tokens of 30 / 60 50 us,

@@ -21,7 +21,9 @@ using namespace diff;
 
 constexpr int kMerge = 64;   // threads of the merge kernel: one key
 
-// dlam of one head: the sum over its rows in all windows, by one workgroup.
+// dlam of one head: the sum over its rows in all windows, by one workgroup.  The other
+// workgroups hide it with three heads and more; 393216 rows of 30 / 60 in windows of 64 take
+// 177 us backward with six heads, 175 with three, but 326 with one.
 template <int NT>
 __device__ inline void sum_dlam(const DiffProblem &p, int h, float *out)
 {
